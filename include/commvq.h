@@ -327,6 +327,118 @@ commvq_status commvq_em_step_shared(const float *data, int32_t group, int32_t n_
                                     float temperature, float *phi, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * ---- Paged caches: block tables and slots, stores, and attention of drafted tokens ----
+ *
+ * A server that appends to many sequences keeps their records in pages of a pool instead of one array per sequence:
+ *   key pages    [n_blocks][Hkv][block_size][M_k] uint8
+ *   value pages  [n_blocks][Hkv][block_size][M_v] uint8
+ *   positions    [n_blocks][block_size][n_axes] int32 (optional)
+ * Token i of sequence b sits in slot  block_tables[b][i / block_size] * block_size + i % block_size.  A step of speculative
+ * decoding is commvq_page_tables (room for the new tokens), commvq_tree_attn (the drafted tree against the pages),
+ * commvq_encode_keys / commvq_encode_values of what was accepted, and commvq_store_pages.
+ *
+ * Rotary positions with several axes (time, height and width of images and video): a token then has n_axes position numbers, and
+ * sub-space j turns by theta_j times the number of its own axis, R_p = diag_j R(p[axis(j)] theta_j).  Codewords commute with every
+ * such R_p (their blocks commute with any rotation of their sub-space), so the cache is read the same way.
+ */
+
+/* Host struct: the pool's geometry. */
+typedef struct {
+    int32_t block_size;  /* tokens of a page: a power of two, 16 .. 1024 */
+    int32_t n_blocks;    /* pages of the pool; n_blocks * block_size < 2^31 */
+    int32_t max_blocks;  /* entries of a row of the block tables (commvq_store_pages does not look at it) */
+    int32_t n_axes;      /* position numbers of a token, 1 .. 4 */
+} commvq_pages;
+
+/* Host struct of device pointers: a batch of sequences with a tree of drafted tokens (nodes) each. */
+typedef struct {
+    int32_t batch;               /* B >= 1 */
+    int32_t total_nodes;         /* N >= 1 rows of q, node_keys, node_vals and out (host copy of cu_nodes[B]) */
+    int32_t max_nodes;           /* host copy of the largest tree, 1 .. 64 */
+    int32_t max_seqlen;          /* host copy of max_b seq_lens[b], >= 0; <= max_blocks * block_size */
+    const int32_t *seq_lens;     /* device [B]: cached tokens of a sequence, >= 0 */
+    const int32_t *block_tables; /* device [B][max_blocks].  Tokens of a page outside 0 .. n_blocks - 1 are left out */
+    const int32_t *cu_nodes;     /* device [B+1]: prefix sums of the sequences' node counts (0 is allowed) */
+    const int32_t *node_pos;     /* device [N][n_axes]: positions of the nodes */
+    const uint64_t *node_mask;   /* device [N] or NULL.  Bit j: the node attends to node j of its own sequence (its own bit
+                                    included or not); bits past the sequence's last node are ignored.  NULL: node i attends to
+                                    0 .. i, a chain */
+    const int32_t *key_pos;      /* device: the pool's positions [n_blocks * block_size][n_axes], or NULL: token i of a sequence
+                                    sits at position i of every axis */
+    const uint8_t *pair_axis;    /* HOST [64], or NULL if n_axes is 1: axis of sub-space j */
+    int32_t q_stride;            /* elements from one node's queries to the next one's; 0: Hq * d (packed) */
+    int32_t node_stride;         /* the same for node_keys and node_vals; 0: Hkv * d */
+} commvq_tree;
+
+/*
+ * Block tables and slots from the requests' lengths, on the GPU.  Request b holds cached_lens[b] tokens in
+ * ceil(cached / block_size) pages and gets new_lens[b] more; pages that it lacks are taken from the front of free_blocks, request
+ * by request.  A request is granted if its row and what is left of the list are long enough (the pages asked for by the
+ * requests before it count whether they were granted or not, so that the order of grants is that of the requests) and if its tokens
+ * end at or before n_slots; a request that is not granted keeps its row and its length, and its new tokens have no slot.
+ *   cached_lens, new_lens  device [B] (negative numbers count as 0)
+ *   free_blocks            device [n_free] (NULL if n_free is 0)
+ *   block_tables           device [B][max_blocks], in/out: entries of new pages are written, all others left as they were
+ *   seq_lens               device [B] out: cached + new where granted, cached otherwise
+ *   cu_new                 device [B+1] out: prefix sums of new_lens (of granted and other requests)
+ *   slots                  device [n_slots] out: slot of every new token, request by request; -1 without one, and behind the last token
+ *   token_pos              device [n_slots] out or NULL: index of every new token in its sequence; behind the last one left as it was
+ *   taken                  device [2] out: pages taken, requests not granted
+ * Outputs must not overlap inputs (block_tables apart).  No handle and no workspace; n_axes is not looked at.
+ */
+commvq_status commvq_page_tables(const commvq_pages *pages, int32_t batch, const int32_t *cached_lens, const int32_t *new_lens,
+                                 const int32_t *free_blocks, int32_t n_free, int32_t *block_tables, int32_t *seq_lens,
+                                 int32_t *cu_new, int32_t *slots, int32_t *token_pos, int32_t n_slots, int32_t *taken,
+                                 void *stream);
+
+/*
+ * Writes the records of n_tokens tokens (and their positions) to their slots.
+ *   slots      device [n_tokens]; a token whose slot is outside the pool (-1) is skipped.  Slots of one call are distinct
+ *              (where two tokens have the same one, its bytes come from one or the other, 16 at a time)
+ *   key_codes  device [n_tokens][Hkv][M_k], val_codes [n_tokens][Hkv][M_v]; 16-byte aligned, as are the pages
+ *   token_pos  device [n_tokens][n_axes] with page_pos, or both NULL
+ * Records in index form only (COMMVQ_ERR_CONFIG otherwise).
+ */
+commvq_status commvq_store_pages(commvq_handle *handle, const commvq_pages *pages, int32_t n_tokens, const int32_t *slots,
+                                 const uint8_t *key_codes, const uint8_t *val_codes, const int32_t *token_pos,
+                                 uint8_t *key_pages, uint8_t *val_pages, int32_t *page_pos, void *stream);
+
+/*
+ * Attention of drafted tokens over a paged compressed cache.  Node i of sequence b (at position t_i) attends to all cached
+ * tokens of its sequence and to the nodes j that its mask names, whose keys and values are given as they are:
+ *     out[i][h] = Softmax over both of ( (q_i R_t_i) . (k R_p) * scale ) . v
+ * with k, v the decoded cache as in commvq_decode_attn, or node_keys[j], node_vals[j] (keys before RoPE).  One node per sequence
+ * is single-token decoding over pages.  A node that attends to nothing gets zeros, rows of out behind the last sequence's nodes are left as they were; keys and values of nodes that a node does not
+ * attend to do not touch it, whatever they hold.
+ *   q                    [N][Hq][d], q_dtype;  node_keys, node_vals  [N][Hkv][d], q_dtype;  out  [N][Hq][d], q_dtype
+ *   key_pages, val_pages as above;  key_codebooks, val_codebooks  as for commvq_decode_attn in index form
+ *   tables               what commvq_tree_prepare made of the codebooks, or NULL: rows are then gathered from the codebooks,
+ *                        whatever the context's length (long ones are several times faster with tables)
+ *   workspace            >= commvq_tree_workspace_bytes(...) bytes, 256-byte aligned, contents undefined after
+ * All data pointers are 16-byte aligned, strides multiples of 8 elements.  Distances between any two positions of a sequence (node or
+ * token, on one axis) must not exceed max_position; beyond, rotations are wrong, but nothing faults.  position_free handles turn nothing.
+ * bf16 queries with bf16 codebooks: decoded and turned keys, turned queries, softmax weights and decoded values are rounded to
+ * bf16 before the products (as a bf16 cache would hold them), all sums are fp32; any other types: fp32 throughout.
+ * COMMVQ_ERR_CONFIG for paired keys and binary values.  Bit-reproducible; concurrent calls need distinct workspaces.
+ */
+commvq_status commvq_tree_workspace_bytes(const commvq_handle *handle, int32_t batch, int32_t total_nodes, int32_t max_nodes,
+                                          int32_t max_seqlen, size_t *bytes);
+commvq_status commvq_tree_attn(commvq_handle *handle, const commvq_pages *pages, const commvq_tree *tree, const void *q,
+                               const void *node_keys, const void *node_vals, const uint8_t *key_pages,
+                               const uint8_t *val_pages, const void *key_codebooks, const void *val_codebooks,
+                               const void *tables, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One-time copy of a layer's static codebooks in the order in which commvq_tree_attn streams them: `tables` is a device buffer
+ * of commvq_tree_table_bytes() bytes, 16-byte aligned, made anew whenever the codebooks change.  bf16 codebooks (COMMVQ_ERR_CONFIG
+ * for fp32 ones: their rows are gathered, pass NULL).  Nothing is remembered: calls get `tables` beside the codebooks,
+ * which short contexts go on reading.
+ */
+commvq_status commvq_tree_table_bytes(const commvq_handle *handle, size_t *bytes);
+commvq_status commvq_tree_prepare(commvq_handle *handle, const void *key_codebooks, const void *val_codebooks, void *tables,
+                                  void *stream);
+
+/*
  * The three stages of commvq_decode_attn, callable on their own (tests and profiling), with the same bits.  (The whole call
  * runs stage two and the product of stage three as one kernel for indexed values; called on their own they pass the bins on
  * through the workspace.)

@@ -38,6 +38,16 @@ class Plan(Structure):
                 ("score_slice_groups", c_int32)]
 
 
+class Pages(Structure):
+    _fields_ = [("block_size", c_int32), ("n_blocks", c_int32), ("max_blocks", c_int32), ("n_axes", c_int32)]
+
+
+class Tree(Structure):
+    _fields_ = [("batch", c_int32), ("total_nodes", c_int32), ("max_nodes", c_int32), ("max_seqlen", c_int32), ("seq_lens", c_void_p),
+                ("block_tables", c_void_p), ("cu_nodes", c_void_p), ("node_pos", c_void_p), ("node_mask", c_void_p), ("key_pos", c_void_p),
+                ("pair_axis", c_void_p), ("q_stride", c_int32), ("node_stride", c_int32)]
+
+
 Handle = c_void_p
 
 EXPORTS = ("commvq_create", "commvq_create_planner", "commvq_destroy", "commvq_validate_config", "commvq_plan_query", "commvq_workspace_bytes",
@@ -47,6 +57,7 @@ EXPORTS = ("commvq_create", "commvq_create_planner", "commvq_destroy", "commvq_v
            "commvq_encoder_table_bytes", "commvq_encoder_prepare", "commvq_encode_keys",
            "commvq_value_encoder_table_bytes", "commvq_value_encoder_prepare", "commvq_encode_values",
            "commvq_em_workspace_bytes", "commvq_em_step", "commvq_em_shared_workspace_bytes", "commvq_em_step_shared",
+           "commvq_page_tables", "commvq_store_pages", "commvq_tree_workspace_bytes", "commvq_tree_attn", "commvq_tree_table_bytes", "commvq_tree_prepare",
            "commvq_profile_enable", "commvq_profile_read", "commvq_status_string")
 
 
@@ -95,6 +106,15 @@ def load_library():
     lib.commvq_em_step.argtypes = [c_void_p, c_int32, c_int32, c_int32, c_float, c_void_p, c_void_p, c_size_t, c_void_p]
     lib.commvq_em_shared_workspace_bytes.argtypes = [c_int32, c_int32, c_int32, POINTER(c_size_t)]
     lib.commvq_em_step_shared.argtypes = [c_void_p, c_int32, c_int32, c_int32, c_float, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.commvq_page_tables.argtypes = [POINTER(Pages), c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
+                                       c_void_p, c_int32, c_void_p, c_void_p]
+    lib.commvq_store_pages.argtypes = [c_void_p, POINTER(Pages), c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                       c_void_p]
+    lib.commvq_tree_workspace_bytes.argtypes = [c_void_p, c_int32, c_int32, c_int32, c_int32, POINTER(c_size_t)]
+    lib.commvq_tree_attn.argtypes = [c_void_p, POINTER(Pages), POINTER(Tree), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                     c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.commvq_tree_table_bytes.argtypes = [c_void_p, POINTER(c_size_t)]
+    lib.commvq_tree_prepare.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
     lib.commvq_profile_enable.argtypes = [c_void_p, c_int32]
     lib.commvq_profile_read.argtypes = [c_void_p, POINTER(c_float), POINTER(c_int32)]
     for name in EXPORTS:
@@ -274,6 +294,62 @@ def commvq_em_step_shared(data, group: int, n_points: int, n_centres: int, tempe
     _check(load_library().commvq_em_step_shared(_ptr(data), int(group), int(n_points), int(n_centres), float(temperature),
                                                 _ptr(phi), _ptr(workspace), int(workspace_bytes), stream or None),
            "commvq_em_step_shared")
+
+
+def make_pages(block_size, n_blocks, max_blocks, n_axes=1) -> Pages:
+    return Pages(int(block_size), int(n_blocks), int(max_blocks), int(n_axes))
+
+
+def make_tree(batch, total_nodes, max_nodes, max_seqlen, seq_lens, block_tables, cu_nodes, node_pos, node_mask=None, key_pos=None, pair_axis=None,
+              q_stride=0, node_stride=0) -> Tree:
+    """Device tensors and host sizes; pair_axis: 64 axis numbers on the host (None with one axis)."""
+    axis = None
+    if pair_axis is not None:
+        axis = (ctypes.c_uint8 * len(pair_axis))(*[int(a) for a in pair_axis])
+        if len(pair_axis) != 64:
+            raise ValueError("pair_axis holds one axis number for each of the 64 sub-spaces")
+    t = Tree(int(batch), int(total_nodes), int(max_nodes), int(max_seqlen), _ptr(seq_lens), _ptr(block_tables), _ptr(cu_nodes), _ptr(node_pos),
+             _ptr(node_mask), _ptr(key_pos), None if axis is None else ctypes.addressof(axis), int(q_stride), int(node_stride))
+    t.kept = axis  # the host array lives as long as the struct
+    return t
+
+
+def commvq_page_tables(pages: Pages, batch: int, cached_lens, new_lens, free_blocks, n_free: int, block_tables, seq_lens, cu_new, slots, token_pos,
+                       n_slots: int, taken, stream: int = 0) -> None:
+    _check(load_library().commvq_page_tables(byref(pages), int(batch), _ptr(cached_lens), _ptr(new_lens), _ptr(free_blocks), int(n_free),
+                                             _ptr(block_tables), _ptr(seq_lens), _ptr(cu_new), _ptr(slots), _ptr(token_pos), int(n_slots),
+                                             _ptr(taken), stream or None), "commvq_page_tables")
+
+
+def commvq_store_pages(handle, pages: Pages, n_tokens: int, slots, key_codes, val_codes, token_pos, key_pages, val_pages, page_pos,
+                       stream: int = 0) -> None:
+    _check(load_library().commvq_store_pages(handle, byref(pages), int(n_tokens), _ptr(slots), _ptr(key_codes), _ptr(val_codes), _ptr(token_pos),
+                                             _ptr(key_pages), _ptr(val_pages), _ptr(page_pos), stream or None), "commvq_store_pages")
+
+
+def commvq_tree_workspace_bytes(handle, batch: int, total_nodes: int, max_nodes: int, max_seqlen: int) -> int:
+    n = c_size_t()
+    _check(load_library().commvq_tree_workspace_bytes(handle, int(batch), int(total_nodes), int(max_nodes), int(max_seqlen), byref(n)),
+           "commvq_tree_workspace_bytes")
+    return int(n.value)
+
+
+def commvq_tree_attn(handle, pages: Pages, tree: Tree, q, node_keys, node_vals, key_pages, val_pages, key_codebooks, val_codebooks, tables, out,
+                     workspace, workspace_bytes: int, stream: int = 0) -> None:
+    _check(load_library().commvq_tree_attn(handle, byref(pages), byref(tree), _ptr(q), _ptr(node_keys), _ptr(node_vals), _ptr(key_pages),
+                                           _ptr(val_pages), _ptr(key_codebooks), _ptr(val_codebooks), _ptr(tables), _ptr(out), _ptr(workspace),
+                                           int(workspace_bytes), stream or None), "commvq_tree_attn")
+
+
+def commvq_tree_table_bytes(handle) -> int:
+    n = c_size_t()
+    _check(load_library().commvq_tree_table_bytes(handle, byref(n)), "commvq_tree_table_bytes")
+    return int(n.value)
+
+
+def commvq_tree_prepare(handle, key_codebooks, val_codebooks, tables, stream: int = 0) -> None:
+    _check(load_library().commvq_tree_prepare(handle, _ptr(key_codebooks), _ptr(val_codebooks), _ptr(tables), stream or None),
+           "commvq_tree_prepare")
 
 
 def commvq_stage_scores(handle, q, key_codes, key_codebooks, positions: Positions, workspace, workspace_bytes: int,

@@ -1,0 +1,698 @@
+// Attention of drafted tokens (trees of up to 64 nodes per sequence) over a paged compressed cache.
+//
+// Row r of (sequence b, KV head g) is query head g G + r % G of node r / G; the rows of a KV head share its decoded keys and values.
+// With t0 the position of a sequence's first node, a row's logit with a cached token at position p is
+//     (q R_t) . (k R_p) scale = Re( [q conj E(t - t0)] conj[k conj E(p - t0)] ) scale,   E(m) = exp(i m theta_j) in sub-space j,
+// so that both sides are turned once, by distances that the phase tables cover, and everything after that is a dense product:
+// logits K Q^T, weights exp(logit - max), and weights times V, with the running maximum and sum of a softmax.  A range of a context's tokens
+// leaves an unnormalised row, its maximum and its sum; k_tree_final joins the ranges with the node's own part.
+#include "commvq_internal.hpp"
+
+#include <algorithm>
+
+commvq_status commvq_check_pages(const commvq_pages *p);
+
+namespace {
+
+constexpr int kMaxNodes = 64;
+constexpr int kChunk = 32;            // tokens that a workgroup of k_tree_rows decodes at a time: one k-step of the second product
+constexpr int kRowBytes = 2 * kD + 16;  // decoded rows in LDS: 16 bytes apart in the banks, for reads of 16 rows at one place
+constexpr int kWideChunk = 16;        // tokens of a chunk of k_tree_rows_f32
+constexpr int kWideRow = kD + 4;      // its rows in LDS, in floats
+
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef short short4_t __attribute__((ext_vector_type(4)));
+
+struct TreeArgs {
+    const void *q, *node_k, *node_v;
+    const uint8_t *key_pages, *val_pages;
+    const void *key_cb, *val_cb;
+    const int32_t *seq_lens, *tables, *cu, *node_pos, *key_pos;
+    const unsigned long long *mask;
+    const float2 *tbl_hi, *tbl_lo;
+    float *part;                      // [row][splits][d] unnormalised
+    float2 *stat;                     // [row][splits] (maximum in powers of 2, sum)
+    void *out;
+    unsigned axes[4];                 // axis of sub-space j: bits 2 (j % 16) of word j / 16
+    long long q_stride, node_stride;
+    int batch, Hq, Hkv, G, Mk, Mv, n_hi, n_axes;
+    int block_bits, n_blocks, max_blocks;
+    int total_nodes, max_nodes, max_seqlen;
+    int splits, split_len, row_tiles;
+    int turn;                         // 0: position_free, nothing is turned
+    int q_bf16, cb_bf16;
+    float scale2;                     // softmax scale times log2(e)
+};
+
+// Sequence b's tokens and nodes, whatever the device arrays hold: inside the buffers that the host has described.
+struct Span {
+    int L, n0, n;
+};
+__device__ __forceinline__ Span span_of(const TreeArgs &a, int b)
+{
+    Span s;
+    s.L = min(max(a.seq_lens[b], 0), a.max_seqlen);
+    s.n0 = min(max(a.cu[b], 0), a.total_nodes);
+    s.n = min(min(max(a.cu[b + 1], s.n0), a.total_nodes) - s.n0, a.max_nodes);
+    return s;
+}
+__device__ __forceinline__ int axis_of(const TreeArgs &a, int j) { return (int)(a.axes[j >> 4] >> (2 * (j & 15))) & 3; }
+
+// E(m) of sub-space j, conjugated where `back` says so: a vector z turned by R_m is z conj E(m)
+__device__ __forceinline__ float2 turned_by(const TreeArgs &a, int m, int j)
+{
+    const unsigned d = m < 0 ? 0u - (unsigned)m : (unsigned)m;
+    const float2 h = a.tbl_hi[(size_t)min(d >> kLoBits, (unsigned)(a.n_hi - 1)) * kJ + j], l = a.tbl_lo[(size_t)(d & (kLo - 1)) * kJ + j];
+    const float x = h.x * l.x - h.y * l.y, y = h.x * l.y + h.y * l.x;
+    return make_float2(x, m < 0 ? y : -y);       // conj E(m)
+}
+__device__ __forceinline__ float2 times(float2 a, float2 b) { return make_float2(a.x * b.x - a.y * b.y, a.x * b.y + a.y * b.x); }
+
+__device__ __forceinline__ unsigned pack_bf16(float lo, float hi)
+{
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    const bf16x2_t p = __builtin_convertvector(f2{lo, hi}, bf16x2_t);  // to nearest, ties to even
+    return __builtin_bit_cast(unsigned, p);
+}
+
+// 4 bf16 of column l % 16 out of a 4 x 16 block of rows that the 16 lanes around l point at, 8 bytes each, row by row
+typedef __attribute__((address_space(3))) short4_t *lds_s4_ptr;
+__device__ __forceinline__ uint2_t lds_read_columns(const void *p)
+{
+    const short4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_ptr)(p));
+    return __builtin_bit_cast(uint2_t, v);
+}
+
+// first operand of the gather sums (see k_score_stream): rows 0..7 add element i of the four lanes' first pieces, rows 8..15 of their second
+__device__ __forceinline__ void selection(int lane, uint4_t &sel, unsigned &sidx)
+{
+    const int n = lane & 15, gk = lane >> 4, e = n & 7, t = e >> 2, pos = e & 3, other = pos == 0 ? 1 : 0;
+    sel = uint4_t{0u, 0u, 0u, 0u};
+    sidx = 0x44444444u;
+    if ((n < 8) == (gk < 2)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if ((i & 1) == t) sel[i] = 0x00003f80u;
+        const unsigned pair = (unsigned)pos | (unsigned)other << 2;
+        sidx = (sidx & ~(0xfu << (4 * t)) & ~(0xfu << (4 * (2 + t)))) | pair << (4 * t) | pair << (4 * (2 + t));
+        sidx = (sidx & 0xffffu) | sidx << 16;
+    }
+}
+
+// ------------------------------------------------------------------ k_tree_rows
+// One range of a context for 16 NR RG rows of a KV head: NR wavefronts with RG tiles of 16 rows each share 32 decoded tokens at a time.
+// Decode: the four 16-lane rows of a wavefront hold four codebooks, a lane a 16-byte piece of a codeword; two tokens' pieces
+// are the dense operand of v_smfmac_f32_16x16x64_bf16, whose constant 0/1 operand adds them in fp32 (exactly: products with 1.0).
+// A lane then has four elements of one token, turns them (keys), rounds them to bf16, as a cache of bf16 keys and values
+// would, and leaves them in LDS.  Products: K Q^T with tokens as rows, so that a lane has 4 tokens of one query row; what it
+// makes of them is, without any exchange, the operand of V^T P^T, whose other operand is read from LDS by columns.
+// Bound by the codeword rows' way through the L1s, 256 bytes a codebook and token; taken for contexts that the streamed kernel's 2 MiB of
+// codebooks per workgroup do not pay for.
+template <int NR, int RG, bool AXES>
+__global__ __launch_bounds__(64 * NR) void k_tree_rows(const TreeArgs a)
+{
+    __shared__ __align__(16) char ktile[kChunk * kRowBytes], vtile[kChunk * kRowBytes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int id = blockIdx.x;
+    const int g = id % a.Hkv;
+    id /= a.Hkv;
+    const int rt = id % a.row_tiles;
+    id /= a.row_tiles;
+    const int split = id % a.splits, b = id / a.splits;
+    const Span s = span_of(a, b);
+    const int R = s.n * a.G, r0 = rt * 16 * NR * RG, t_begin = split * a.split_len, t_end = min(s.L, t_begin + a.split_len);
+    if (r0 >= R || t_begin >= t_end) return;
+    const int n = lane & 15, gk = lane >> 4;
+
+    int t0[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+        if (a.turn && x < a.n_axes) t0[x] = a.node_pos[(size_t)s.n0 * a.n_axes + x];
+    auto origin = [&](int ax) { return !AXES || ax == 0 ? t0[0] : ax == 1 ? t0[1] : ax == 2 ? t0[2] : t0[3]; };
+
+    // queries, turned and scaled, as second operand: row n, elements 32 ks + 8 gk ..
+    uint4_t qv[RG][4];
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+        const int r = r0 + (wave * RG + rg) * 16 + n;
+        const int node = r / a.G, h = r % a.G;
+        const bool there = r < R;
+        const size_t at = (size_t)(s.n0 + (there ? node : 0)) * a.q_stride + (size_t)(g * a.G + h) * kD;
+        const int32_t *pos = a.node_pos + (size_t)(s.n0 + (there ? node : 0)) * a.n_axes;
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            const uint4_t raw = *reinterpret_cast<const uint4_t *>(static_cast<const uint16_t *>(a.q) + at + 32 * ks + 8 * gk);
+            uint4_t w;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int j = 16 * ks + 4 * gk + u, ax = AXES ? axis_of(a, j) : 0;
+                float2 z = make_float2(bf16_lo(raw[u]), bf16_hi(raw[u]));
+                if (a.turn) z = times(z, turned_by(a, pos[ax] - origin(ax), j));
+                w[u] = there ? pack_bf16(z.x * a.scale2, z.y * a.scale2) : 0u;
+            }
+            qv[rg][ks] = w;
+        }
+    }
+
+    uint4_t sel;
+    unsigned sidx;
+    selection(lane, sel, sidx);
+    const bf16x8_t selv = __builtin_bit_cast(bf16x8_t, sel);
+    const int half = gk & 1, second = gk >> 1;      // the lane's 4 elements of a piece, and which token of a pair it ends up with
+    const __amdgpu_buffer_rsrc_t krows = make_rsrc(static_cast<const uint16_t *>(a.key_cb) + (size_t)g * a.Mk * kK * kD, (unsigned)(a.Mk * kK * kD * 2));
+    const __amdgpu_buffer_rsrc_t vrows = make_rsrc(static_cast<const uint16_t *>(a.val_cb) + (size_t)g * a.Mv * kK * kD, (unsigned)(a.Mv * kK * kD * 2));
+    const unsigned lane_at = (unsigned)(4 * gk) * (kK * kD * 2) + (unsigned)n * 16u;
+    const int32_t *table = a.tables + (size_t)b * a.max_blocks;
+
+    floatx4_t o[RG][8];                              // element 16 x + 4 gk + i of row n
+    float m[RG], l[RG];
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+        m[rg] = -INFINITY;
+        l[rg] = 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) o[rg][x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    }
+
+    constexpr int PER = kChunk / NR;                 // tokens that a wavefront decodes
+    for (int c0 = t_begin; c0 < t_end; c0 += kChunk) {
+        const int tok = c0 + (lane & (kChunk - 1));
+        int page = tok < t_end ? table[tok >> a.block_bits] : -1;
+        const bool there = page >= 0 && page < a.n_blocks;
+        const unsigned seen = (unsigned)__ballot(there);   // (both halves of the wavefront hold the 32 tokens)
+        page = there ? page : 0;                     // any page does for a token that is not counted
+        // the sums of the two tokens at first + 2 pair, first the first one's
+        auto decode = [&](const uint8_t *pages, int M, const __amdgpu_buffer_rsrc_t rows, int i) {
+            floatx4_t acc = {0.f, 0.f, 0.f, 0.f};
+            const int pa = __builtin_amdgcn_readlane(page, i), pb = __builtin_amdgcn_readlane(page, i + 1);
+            const int in_page = (1 << a.block_bits) - 1;
+            const uint8_t *ca = pages + ((((size_t)pa * a.Hkv + g) << a.block_bits) + ((c0 + i) & in_page)) * M + 4 * gk;
+            const uint8_t *cb = pages + ((((size_t)pb * a.Hkv + g) << a.block_bits) + ((c0 + i + 1) & in_page)) * M + 4 * gk;
+            for (int blk = 0; blk < M; blk += 16) {
+                const unsigned wa = *reinterpret_cast<const unsigned *>(ca + blk), wb = *reinterpret_cast<const unsigned *>(cb + blk);
+                uint4_t va[4], vb[4];
+#pragma unroll
+                for (int st = 0; st < 4; ++st) {
+                    const int row = (blk + st) * (kK * kD * 2);
+                    va[st] = __builtin_amdgcn_raw_buffer_load_b128(rows, lane_at + ((wa >> (8 * st) & 255u) << 8), row, 0);
+                    vb[st] = __builtin_amdgcn_raw_buffer_load_b128(rows, lane_at + ((wb >> (8 * st) & 255u) << 8), row, 0);
+                }
+#pragma unroll
+                for (int st = 0; st < 4; ++st) {
+                    const uint8v_t both = {va[st][0], va[st][1], va[st][2], va[st][3], vb[st][0], vb[st][1], vb[st][2], vb[st][3]};
+                    acc = __builtin_amdgcn_smfmac_f32_16x16x64_bf16(selv, __builtin_bit_cast(bf16x16_t, both), acc, (int)sidx, 0, 0);
+                }
+            }
+            return acc;
+        };
+#pragma unroll 2
+        for (int p = 0; p < PER; p += 2) {
+            const int i = wave * PER + p;
+            floatx4_t k = decode(a.key_pages, a.Mk, krows, i);
+            const int mine = i + second;
+            if (a.turn) {
+                const int j = 4 * n + 2 * half;
+                int pos = c0 + mine;
+                const int32_t *own = nullptr;
+                if (a.key_pos) {
+                    const int pg = second ? __builtin_amdgcn_readlane(page, i + 1) : __builtin_amdgcn_readlane(page, i);
+                    own = a.key_pos + (((size_t)pg << a.block_bits) + (pos & ((1 << a.block_bits) - 1))) * a.n_axes;
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int ax = AXES ? axis_of(a, j + u) : 0;
+                    const float2 z = times(make_float2(k[2 * u], k[2 * u + 1]), turned_by(a, (own ? own[ax] : pos) - origin(ax), j + u));
+                    k[2 * u] = z.x;
+                    k[2 * u + 1] = z.y;
+                }
+            }
+            *reinterpret_cast<uint2_t *>(ktile + mine * kRowBytes + n * 16 + half * 8) = uint2_t{pack_bf16(k[0], k[1]), pack_bf16(k[2], k[3])};
+        }
+        __syncthreads();
+        floatx4_t sc[RG][2];
+#pragma unroll
+        for (int rg = 0; rg < RG; ++rg) sc[rg][0] = sc[rg][1] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const uint4_t kv = *reinterpret_cast<const uint4_t *>(ktile + (16 * t + n) * kRowBytes + 64 * ks + 16 * gk);
+#pragma unroll
+                for (int rg = 0; rg < RG; ++rg)
+                    sc[rg][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kv), __builtin_bit_cast(bf16x8_t, qv[rg][ks]), sc[rg][t], 0, 0, 0);
+            }
+#pragma unroll 2
+        for (int p = 0; p < PER; p += 2) {
+            const int i = wave * PER + p, mine = i + second;
+            const floatx4_t v = decode(a.val_pages, a.Mv, vrows, i);
+            const bool counts = seen >> mine & 1u;   // (a weight of zero does not hide an infinity)
+            *reinterpret_cast<uint2_t *>(vtile + mine * kRowBytes + n * 16 + half * 8) =
+                uint2_t{counts ? pack_bf16(v[0], v[1]) : 0u, counts ? pack_bf16(v[2], v[3]) : 0u};
+        }
+        uint4_t pv[RG];
+#pragma unroll
+        for (int rg = 0; rg < RG; ++rg) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (!(seen >> (16 * t + 4 * gk + i) & 1u)) sc[rg][t][i] = -INFINITY;
+                    top = fmaxf(top, sc[rg][t][i]);
+                }
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float now = fmaxf(m[rg], top), base = now == -INFINITY ? 0.f : now;
+            const float old = __builtin_amdgcn_exp2f(m[rg] - base);
+            m[rg] = now;
+            float sum = 0.f, w[8];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    w[4 * t + i] = __builtin_amdgcn_exp2f(sc[rg][t][i] - base);
+                    sum += w[4 * t + i];
+                }
+            l[rg] = l[rg] * old + sum;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pv[rg][i] = pack_bf16(w[2 * i], w[2 * i + 1]);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) o[rg][x] *= old;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const char *at = vtile + (4 * gk + n / 4) * kRowBytes + 32 * x + 8 * (n & 3);
+            const uint2_t v0 = lds_read_columns(at), v1 = lds_read_columns(at + 16 * kRowBytes);
+            const uint4_t vv = {v0[0], v0[1], v1[0], v1[1]};
+#pragma unroll
+            for (int rg = 0; rg < RG; ++rg)
+                o[rg][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vv), __builtin_bit_cast(bf16x8_t, pv[rg]), o[rg][x], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int rg = 0; rg < RG; ++rg) {
+        float sum = l[rg];
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        const int r = r0 + (wave * RG + rg) * 16 + n;
+        if (r >= R) continue;
+        const size_t row = ((size_t)(s.n0 + r / a.G) * a.Hq + g * a.G + r % a.G) * a.splits + split;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) *reinterpret_cast<floatx4_t *>(a.part + row * kD + 16 * x + 4 * gk) = o[rg][x];
+        if (gk == 0) a.stat[row] = make_float2(m[rg], sum);
+    }
+}
+
+// ------------------------------------------------------------------ k_tree_rows_f32
+// The same in fp32 throughout, for fp32 queries or codebooks: four wavefronts with 16 rows each, 16 tokens at a time.  A thread decodes 8
+// elements of a token by vector additions; products by v_mfma_f32_16x16x4_f32, whose operands have one element a lane, so that
+// a weight is an operand of the second product as it is.
+template <bool Q16, bool CB16>
+__global__ __launch_bounds__(256) void k_tree_rows_f32(const TreeArgs a)
+{
+    __shared__ __align__(16) float ktile[kWideChunk * kWideRow], vtile[kWideChunk * kWideRow];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int id = blockIdx.x;
+    const int g = id % a.Hkv;
+    id /= a.Hkv;
+    const int rt = id % a.row_tiles;
+    id /= a.row_tiles;
+    const int split = id % a.splits, b = id / a.splits;
+    const Span s = span_of(a, b);
+    const int R = s.n * a.G, r0 = rt * 64, t_begin = split * a.split_len, t_end = min(s.L, t_begin + a.split_len);
+    if (r0 >= R || t_begin >= t_end) return;
+    const int n = lane & 15, gk = lane >> 4;
+    const int r = r0 + wave * 16 + n;
+    const bool row_there = r < R;
+    const int node = s.n0 + (row_there ? r / a.G : 0), h = r % a.G;
+
+    // row n, element 4 x + gk
+    float qv[32];
+#pragma unroll
+    for (int x = 0; x < 32; ++x) {
+        const int e = 4 * x + gk, j = e >> 1, ax = axis_of(a, j);
+        const size_t at = (size_t)node * a.q_stride + (size_t)(g * a.G + h) * kD + 2 * j;
+        float2 z = make_float2(cb_elem<Q16>(a.q, at), cb_elem<Q16>(a.q, at + 1));
+        if (a.turn) z = times(z, turned_by(a, a.node_pos[(size_t)node * a.n_axes + ax] - a.node_pos[(size_t)s.n0 * a.n_axes + ax], j));
+        qv[x] = row_there ? (e & 1 ? z.y : z.x) * a.scale2 : 0.f;
+    }
+    floatx4_t o[8];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) o[x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+    const int32_t *table = a.tables + (size_t)b * a.max_blocks;
+    const int dt = tid >> 4, de = (tid & 15) * 8;   // the token and elements that this thread decodes
+    for (int c0 = t_begin; c0 < t_end; c0 += kWideChunk) {
+        const int tok = c0 + (lane & 15);
+        const int pg = tok < t_end ? table[tok >> a.block_bits] : -1;
+        const unsigned seen = (unsigned)__ballot(pg >= 0 && pg < a.n_blocks) & 0xffffu;
+        const bool counts = seen >> dt & 1u;
+        const int page = counts ? table[(c0 + dt) >> a.block_bits] : 0, in_page = (c0 + dt) & ((1 << a.block_bits) - 1);
+        const size_t rec = (((size_t)page * a.Hkv + g) << a.block_bits) + in_page;
+        auto decode = [&](const uint8_t *codes, const void *cb, int M, float *acc) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+            for (int c = 0; c < M; c += 4) {
+                const unsigned w = *reinterpret_cast<const unsigned *>(codes + c);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const size_t at = (((size_t)g * M + c + u) * kK + (w >> (8 * u) & 255u)) * kD + de;
+                    if constexpr (CB16) {
+                        const uint4_t x = *reinterpret_cast<const uint4_t *>(static_cast<const uint16_t *>(cb) + at);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { acc[2 * e] += bf16_lo(x[e]); acc[2 * e + 1] += bf16_hi(x[e]); }
+                    } else {
+                        const floatx4_t x = *reinterpret_cast<const floatx4_t *>(static_cast<const float *>(cb) + at);
+                        const floatx4_t y = *reinterpret_cast<const floatx4_t *>(static_cast<const float *>(cb) + at + 4);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { acc[e] += x[e]; acc[4 + e] += y[e]; }
+                    }
+                }
+            }
+        };
+        float x[8];
+        decode(a.key_pages + rec * a.Mk, a.key_cb, a.Mk, x);
+        if (a.turn) {
+            const int32_t *own = a.key_pos ? a.key_pos + (((size_t)page << a.block_bits) + in_page) * a.n_axes : nullptr;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int j = de / 2 + u, ax = axis_of(a, j);
+                const float2 z = times(make_float2(x[2 * u], x[2 * u + 1]), turned_by(a, (own ? own[ax] : c0 + dt) - a.node_pos[(size_t)s.n0 * a.n_axes + ax], j));
+                x[2 * u] = z.x;
+                x[2 * u + 1] = z.y;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ktile[dt * kWideRow + de + e] = x[e];
+        decode(a.val_pages + rec * a.Mv, a.val_cb, a.Mv, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vtile[dt * kWideRow + de + e] = counts ? x[e] : 0.f;
+        __syncthreads();
+        floatx4_t sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < 32; ++k) sc = __builtin_amdgcn_mfma_f32_16x16x4f32(ktile[n * kWideRow + 4 * k + gk], qv[k], sc, 0, 0, 0);
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (!(seen >> (4 * gk + i) & 1u)) sc[i] = -INFINITY;
+            top = fmaxf(top, sc[i]);
+        }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float now = fmaxf(m, top), base = now == -INFINITY ? 0.f : now, old = __builtin_amdgcn_exp2f(m - base);
+        m = now;
+        float w[4], sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { w[i] = __builtin_amdgcn_exp2f(sc[i] - base); sum += w[i]; }
+        l = l * old + sum;
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+            o[y] *= old;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[y] = __builtin_amdgcn_mfma_f32_16x16x4f32(vtile[(4 * gk + i) * kWideRow + 16 * y + n], w[i], o[y], 0, 0, 0);
+        }
+        __syncthreads();
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (!row_there) return;
+    const size_t row = ((size_t)node * a.Hq + g * a.G + h) * a.splits + split;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) *reinterpret_cast<floatx4_t *>(a.part + row * kD + 16 * y + 4 * gk) = o[y];
+    if (gk == 0) a.stat[row] = make_float2(m, l);
+}
+
+// ------------------------------------------------------------------ k_tree_final
+constexpr int kFinalWaves = 4;
+
+// A workgroup joins the parts of one row: a wavefront every fourth range and every fourth node that the row attends to, a lane one
+// sub-space.  The nodes' part is fp32 arithmetic, node by node: nodes outside the mask are not read, so that what they hold cannot matter.
+template <bool Q16>
+__global__ __launch_bounds__(64 * kFinalWaves) void k_tree_final(const TreeArgs a)
+{
+    __shared__ float sm[kFinalWaves], sl[kFinalWaves];
+    __shared__ float2 so[kFinalWaves][kJ];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int node = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, g = h / a.G;
+    // the sequence: as many as end at or before this node come before it
+    int b = 0;
+    for (int c = 0; c < a.batch; c += 64) {
+        const int x = c + lane;
+        const int ended = __popcll(__ballot(x < a.batch && a.cu[x + 1] <= node));
+        b += ended;
+        if (ended < 64) break;
+    }
+    if (b >= a.batch) return;                         // a row behind the last sequence
+    float m = -INFINITY, l = 0.f;
+    float2 o = make_float2(0.f, 0.f);
+    {
+        const Span s = span_of(a, b);
+        const int i = node - s.n0;
+        if (i >= 0 && i < s.n) {
+            const int ns = (s.L + a.split_len - 1) / a.split_len;
+            const size_t row = (size_t)blockIdx.x * a.splits;
+            for (int k = wave; k < ns; k += kFinalWaves) {
+                const float2 st = a.stat[row + k];
+                const float2 v = *reinterpret_cast<const float2 *>(a.part + (row + k) * kD + 2 * lane);
+                if (st.x == -INFINITY) continue;      // (a range without a page)
+                const float now = fmaxf(m, st.x), x = __builtin_amdgcn_exp2f(m - now), y = __builtin_amdgcn_exp2f(st.x - now);
+                m = now;
+                l = l * x + st.y * y;
+                o.x = o.x * x + v.x * y;
+                o.y = o.y * x + v.y * y;
+            }
+            unsigned long long mask = a.mask ? a.mask[node] : ~0ull >> (63 - i);
+            if (s.n < 64) mask &= (1ull << s.n) - 1;
+            const int ax = axis_of(a, lane);
+            const size_t at = (size_t)node * a.q_stride + (size_t)h * kD + 2 * lane;
+            const float2 q = make_float2(cb_elem<Q16>(a.q, at) * a.scale2, cb_elem<Q16>(a.q, at + 1) * a.scale2);
+            const int own = a.turn ? a.node_pos[(size_t)node * a.n_axes + ax] : 0;
+            for (int k = 0; mask; mask &= mask - 1, ++k) {
+                if (k % kFinalWaves != wave) continue;
+                const int j = s.n0 + __builtin_ctzll(mask);
+                const size_t from = (size_t)j * a.node_stride + (size_t)g * kD + 2 * lane;
+                const float2 key = make_float2(cb_elem<Q16>(a.node_k, from), cb_elem<Q16>(a.node_k, from + 1));
+                const float2 val = make_float2(cb_elem<Q16>(a.node_v, from), cb_elem<Q16>(a.node_v, from + 1));
+                float2 z = q;
+                if (a.turn) z = times(q, turned_by(a, own - a.node_pos[(size_t)j * a.n_axes + ax], lane));
+                const float x = wave_sum(z.x * key.x + z.y * key.y);
+                const float now = fmaxf(m, x), base = now == -INFINITY ? 0.f : now;
+                const float was = __builtin_amdgcn_exp2f(m - base), w = __builtin_amdgcn_exp2f(x - base);
+                m = now;
+                l = l * was + w;
+                o.x = o.x * was + val.x * w;
+                o.y = o.y * was + val.y * w;
+            }
+        }
+    }
+    if (lane == 0) { sm[wave] = m; sl[wave] = l; }
+    so[wave][lane] = o;
+    __syncthreads();
+    if (wave) return;
+    float top = -INFINITY, sum = 0.f;
+    float2 t = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kFinalWaves; ++w) top = fmaxf(top, sm[w]);
+#pragma unroll
+    for (int w = 0; w < kFinalWaves; ++w) {
+        if (sl[w] == 0.f) continue;                   // (nothing there)
+        const float f = __builtin_amdgcn_exp2f(sm[w] - top);
+        sum += sl[w] * f;
+        t.x += so[w][lane].x * f;
+        t.y += so[w][lane].y * f;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row that attends to nothing: zeros
+    if (Q16) static_cast<unsigned *>(a.out)[(size_t)blockIdx.x * kJ + lane] = pack_bf16(t.x * inv, t.y * inv);
+    else static_cast<float2 *>(a.out)[(size_t)blockIdx.x * kJ + lane] = make_float2(t.x * inv, t.y * inv);
+}
+
+// ------------------------------------------------------------------ k_tree_pack
+// A codebook in the order in which it is streamed through LDS: packed[head][slice][block of 16 books][word][16 books], pieces of 16 bytes,
+// slice = 8 consecutive elements of every codeword.  One thread per piece of the source.
+__global__ __launch_bounds__(256) void k_tree_pack(const uint4 *__restrict__ cb, uint4 *__restrict__ packed, int M, size_t pieces)
+{
+    const size_t t = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (t >= pieces) return;
+    const int sl = (int)(t & 15);
+    const size_t row = t >> 4;                  // (head * M + book) * 256 + word
+    const int word = (int)(row & (kK - 1));
+    const size_t hm = row / kK;
+    const int m = (int)(hm % M);
+    const size_t g = hm / M;
+    packed[(((g * 16 + sl) * (M / 16) + m / 16) * kK + word) * 16 + m % 16] = cb[t];
+}
+
+// ------------------------------------------------------------------ host side
+struct TreePlan {
+    int nr, rg;          // wavefronts and row tiles per wavefront of a workgroup
+    int row_tiles, splits, split_len;
+    size_t stat_at, bytes;
+};
+
+inline bool wide(const commvq_config &c) { return c.q_dtype != COMMVQ_BF16 || c.codebook_dtype != COMMVQ_BF16; }
+
+// Rows of a workgroup: the smallest of 16, 32, 64, 128 and 256 that holds the largest tree's.  Ranges: as many as fill the chip with 16 wavefronts a
+// compute unit, in whole chunks.
+TreePlan tree_plan(const commvq_handle *h, int batch, int total_nodes, int max_nodes, int max_seqlen)
+{
+    TreePlan p{};
+    const int rows = max_nodes * h->G;
+    p.nr = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8;
+    p.rg = rows > 128 ? 2 : 1;
+    if (wide(h->cfg)) { p.nr = 4; p.rg = 1; }
+    p.row_tiles = (rows + 16 * p.nr * p.rg - 1) / (16 * p.nr * p.rg);
+    const int chunk = wide(h->cfg) ? kWideChunk : kChunk;
+    const int64_t units = (int64_t)batch * h->cfg.n_kv_heads * p.row_tiles;
+    const int64_t chunks = (max_seqlen + chunk - 1) / chunk;
+    const int64_t want = std::max<int64_t>(1, 4096 / p.nr / units);
+    const int64_t per = std::max<int64_t>(1, (chunks + want - 1) / want);
+    p.split_len = (int)per * chunk;
+    p.splits = (int)((chunks + per - 1) / per);
+    const size_t parts = (size_t)total_nodes * h->cfg.n_q_heads * p.splits;
+    p.stat_at = align_up(parts * kD * 4, 256);
+    p.bytes = std::max<size_t>(256, align_up(p.stat_at + parts * 8, 256));
+    return p;
+}
+
+commvq_status check_tree_sizes(const commvq_handle *h, int32_t batch, int32_t total_nodes, int32_t max_nodes, int32_t max_seqlen)
+{
+    if (h->cfg.key_format != COMMVQ_KEYS_INDEXED || h->cfg.value_format != COMMVQ_VALUES_INDEXED) return COMMVQ_ERR_CONFIG;
+    if (batch < 1 || max_nodes < 1 || max_nodes > kMaxNodes || total_nodes < max_nodes || (int64_t)total_nodes > (int64_t)batch * max_nodes) return COMMVQ_ERR_SHAPE;
+    if (max_seqlen < 0 || max_seqlen > 1 << 30) return COMMVQ_ERR_SHAPE;
+    if ((int64_t)total_nodes * h->cfg.n_q_heads > 0x7fffffff) return COMMVQ_ERR_SHAPE;  // workgroups of the last kernel
+    return COMMVQ_OK;
+}
+
+template <int NR, int RG>
+hipError_t launch_rows(const TreeArgs &a, dim3 grid, hipStream_t s)
+{
+    if (a.n_axes > 1) k_tree_rows<NR, RG, true><<<grid, 64 * NR, 0, s>>>(a);
+    else k_tree_rows<NR, RG, false><<<grid, 64 * NR, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_wide(const TreeArgs &a, dim3 grid, hipStream_t s)
+{
+    if (a.q_bf16) k_tree_rows_f32<true, false><<<grid, 256, 0, s>>>(a);
+    else if (a.cb_bf16) k_tree_rows_f32<false, true><<<grid, 256, 0, s>>>(a);
+    else k_tree_rows_f32<false, false><<<grid, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+bool misaligned(std::initializer_list<const void *> ps)
+{
+    uintptr_t all = 0;
+    for (const void *p : ps) all |= reinterpret_cast<uintptr_t>(p);
+    return (all & 15u) != 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+commvq_status commvq_tree_workspace_bytes(const commvq_handle *h, int32_t batch, int32_t total_nodes, int32_t max_nodes,
+                                          int32_t max_seqlen, size_t *bytes)
+{
+    if (!h || !bytes) return COMMVQ_ERR_NULL;
+    const commvq_status st = check_tree_sizes(h, batch, total_nodes, max_nodes, max_seqlen);
+    if (st != COMMVQ_OK) return st;
+    *bytes = tree_plan(h, batch, total_nodes, max_nodes, max_seqlen).bytes;
+    return COMMVQ_OK;
+}
+
+commvq_status commvq_tree_attn(commvq_handle *h, const commvq_pages *pages, const commvq_tree *t, const void *q,
+                               const void *node_keys, const void *node_vals, const uint8_t *key_pages,
+                               const uint8_t *val_pages, const void *key_cb, const void *val_cb, const void *tables,
+                               void *out, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!h || !t || !q || !node_keys || !node_vals || !key_pages || !val_pages || !key_cb || !val_cb || !out) return COMMVQ_ERR_NULL;
+    if (!t->seq_lens || !t->block_tables || !t->cu_nodes || !t->node_pos) return COMMVQ_ERR_NULL;
+    commvq_status st = commvq_check_pages(pages);
+    if (st != COMMVQ_OK) return st;
+    if (pages->n_axes > 1 && !t->pair_axis) return COMMVQ_ERR_NULL;
+    st = check_tree_sizes(h, t->batch, t->total_nodes, t->max_nodes, t->max_seqlen);
+    if (st != COMMVQ_OK) return st;
+    const commvq_config &c = h->cfg;
+    if (tables && c.codebook_dtype != COMMVQ_BF16) return COMMVQ_ERR_CONFIG;
+    if ((int64_t)t->max_seqlen > (int64_t)pages->max_blocks * pages->block_size) return COMMVQ_ERR_SHAPE;
+    // keys at positions 0 .. L - 1 and nodes at or after the last of them
+    if (!t->key_pos && !c.position_free && (int64_t)t->max_seqlen - 1 > c.max_position) return COMMVQ_ERR_SHAPE;
+    if (misaligned({q, node_keys, node_vals, key_pages, val_pages, key_cb, val_cb, tables, out})) return COMMVQ_ERR_SHAPE;
+    const int64_t q_row = (int64_t)c.n_q_heads * kD, node_row = (int64_t)c.n_kv_heads * kD;
+    if (t->q_stride && (t->q_stride < q_row || t->q_stride % 8)) return COMMVQ_ERR_SHAPE;
+    if (t->node_stride && (t->node_stride < node_row || t->node_stride % 8)) return COMMVQ_ERR_SHAPE;
+    TreeArgs a{};
+    if (t->pair_axis)
+        for (int j = 0; j < kJ; ++j) {
+            if (t->pair_axis[j] >= pages->n_axes) return COMMVQ_ERR_SHAPE;
+            a.axes[j >> 4] |= (unsigned)t->pair_axis[j] << (2 * (j & 15));
+        }
+    const TreePlan p = tree_plan(h, t->batch, t->total_nodes, t->max_nodes, t->max_seqlen);
+    const int64_t wgs = (int64_t)t->batch * c.n_kv_heads * p.row_tiles * p.splits;
+    if (wgs > 0x7fffffff) return COMMVQ_ERR_SHAPE;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < p.bytes) return COMMVQ_ERR_WORKSPACE;
+    if (h->device < 0) return COMMVQ_ERR_NO_DEVICE;
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess || dev != h->device) return COMMVQ_ERR_NO_DEVICE;  // the phase tables are another GPU's
+    a.q = q; a.node_k = node_keys; a.node_v = node_vals; a.key_pages = key_pages; a.val_pages = val_pages; a.key_cb = key_cb; a.val_cb = val_cb;
+    a.seq_lens = t->seq_lens; a.tables = t->block_tables; a.cu = t->cu_nodes; a.node_pos = t->node_pos; a.key_pos = t->key_pos;
+    a.mask = reinterpret_cast<const unsigned long long *>(t->node_mask);
+    a.tbl_hi = h->tbl_hi; a.tbl_lo = h->tbl_lo;
+    a.part = static_cast<float *>(workspace);
+    a.stat = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + p.stat_at);
+    a.out = out;
+    a.q_stride = t->q_stride ? t->q_stride : q_row; a.node_stride = t->node_stride ? t->node_stride : node_row;
+    a.batch = t->batch; a.Hq = c.n_q_heads; a.Hkv = c.n_kv_heads; a.G = h->G; a.Mk = c.m_key; a.Mv = c.m_val; a.n_hi = h->n_hi;
+    a.n_axes = pages->n_axes; a.block_bits = __builtin_ctz((unsigned)pages->block_size); a.n_blocks = pages->n_blocks; a.max_blocks = pages->max_blocks;
+    a.total_nodes = t->total_nodes; a.max_nodes = t->max_nodes; a.max_seqlen = t->max_seqlen;
+    a.splits = p.splits; a.split_len = p.split_len; a.row_tiles = p.row_tiles;
+    a.turn = !c.position_free; a.q_bf16 = c.q_dtype == COMMVQ_BF16; a.cb_bf16 = c.codebook_dtype == COMMVQ_BF16;
+    a.scale2 = h->scale * kLog2e;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (wgs > 0) {
+        const dim3 grid((unsigned)wgs);
+        hipError_t e;
+        if (wide(c)) e = launch_wide(a, grid, s);
+        else if (p.nr == 1) e = launch_rows<1, 1>(a, grid, s);
+        else if (p.nr == 2) e = launch_rows<2, 1>(a, grid, s);
+        else if (p.nr == 4) e = launch_rows<4, 1>(a, grid, s);
+        else if (p.rg == 1) e = launch_rows<8, 1>(a, grid, s);
+        else e = launch_rows<8, 2>(a, grid, s);
+        if (e != hipSuccess) return COMMVQ_ERR_LAUNCH;
+    }
+    const dim3 rows((unsigned)((int64_t)t->total_nodes * c.n_q_heads));
+    if (a.q_bf16) k_tree_final<true><<<rows, 64 * kFinalWaves, 0, s>>>(a);
+    else k_tree_final<false><<<rows, 64 * kFinalWaves, 0, s>>>(a);
+    return hipGetLastError() == hipSuccess ? COMMVQ_OK : COMMVQ_ERR_LAUNCH;
+}
+
+commvq_status commvq_tree_table_bytes(const commvq_handle *h, size_t *bytes)
+{
+    if (!h || !bytes) return COMMVQ_ERR_NULL;
+    const commvq_config &c = h->cfg;
+    if (c.codebook_dtype != COMMVQ_BF16 || c.key_format != COMMVQ_KEYS_INDEXED || c.value_format != COMMVQ_VALUES_INDEXED) return COMMVQ_ERR_CONFIG;
+    *bytes = (size_t)c.n_kv_heads * (c.m_key + c.m_val) * kK * kD * 2;
+    return COMMVQ_OK;
+}
+
+commvq_status commvq_tree_prepare(commvq_handle *h, const void *key_cb, const void *val_cb, void *tables, void *stream)
+{
+    if (!h || !key_cb || !val_cb || !tables) return COMMVQ_ERR_NULL;
+    size_t bytes = 0;
+    const commvq_status st = commvq_tree_table_bytes(h, &bytes);
+    if (st != COMMVQ_OK) return st;
+    if (misaligned({key_cb, val_cb, tables})) return COMMVQ_ERR_SHAPE;
+    if (h->device < 0) return COMMVQ_ERR_NO_DEVICE;
+    const commvq_config &c = h->cfg;
+    const size_t kp = (size_t)c.n_kv_heads * c.m_key * kK * 16, vp = (size_t)c.n_kv_heads * c.m_val * kK * 16;
+    if (std::max(kp, vp) / 256 > 0x7fffffff) return COMMVQ_ERR_SHAPE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    uint4 *to = static_cast<uint4 *>(tables);
+    k_tree_pack<<<dim3((unsigned)(kp / 256)), 256, 0, s>>>(static_cast<const uint4 *>(key_cb), to, c.m_key, kp);
+    if (hipGetLastError() != hipSuccess) return COMMVQ_ERR_LAUNCH;
+    k_tree_pack<<<dim3((unsigned)(vp / 256)), 256, 0, s>>>(static_cast<const uint4 *>(val_cb), to + kp, c.m_val, vp);
+    return hipGetLastError() == hipSuccess ? COMMVQ_OK : COMMVQ_ERR_LAUNCH;
+}
+
+}  // extern "C"
