@@ -368,6 +368,8 @@ typedef struct {
     const uint8_t *pair_axis;    /* HOST [64], or NULL if n_axes is 1: axis of sub-space j */
     int32_t q_stride;            /* elements from one node's queries to the next one's; 0: Hq * d (packed) */
     int32_t node_stride;         /* the same for node_keys and node_vals; 0: Hkv * d */
+    int64_t total_tokens;        /* host copy of the sum of seq_lens, or 0: not known.  Long ragged batches of many rows are taken in
+                                    fewer steps with it; sequences behind the first total_tokens (in whole tiles of 2048) are not attended to */
 } commvq_tree;
 
 /*

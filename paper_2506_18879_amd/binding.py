@@ -45,7 +45,7 @@ class Pages(Structure):
 class Tree(Structure):
     _fields_ = [("batch", c_int32), ("total_nodes", c_int32), ("max_nodes", c_int32), ("max_seqlen", c_int32), ("seq_lens", c_void_p),
                 ("block_tables", c_void_p), ("cu_nodes", c_void_p), ("node_pos", c_void_p), ("node_mask", c_void_p), ("key_pos", c_void_p),
-                ("pair_axis", c_void_p), ("q_stride", c_int32), ("node_stride", c_int32)]
+                ("pair_axis", c_void_p), ("q_stride", c_int32), ("node_stride", c_int32), ("total_tokens", c_int64)]
 
 
 Handle = c_void_p
@@ -301,7 +301,7 @@ def make_pages(block_size, n_blocks, max_blocks, n_axes=1) -> Pages:
 
 
 def make_tree(batch, total_nodes, max_nodes, max_seqlen, seq_lens, block_tables, cu_nodes, node_pos, node_mask=None, key_pos=None, pair_axis=None,
-              q_stride=0, node_stride=0) -> Tree:
+              q_stride=0, node_stride=0, total_tokens=0) -> Tree:
     """Device tensors and host sizes; pair_axis: 64 axis numbers on the host (None with one axis)."""
     axis = None
     if pair_axis is not None:
@@ -309,7 +309,8 @@ def make_tree(batch, total_nodes, max_nodes, max_seqlen, seq_lens, block_tables,
         if len(pair_axis) != 64:
             raise ValueError("pair_axis holds one axis number for each of the 64 sub-spaces")
     t = Tree(int(batch), int(total_nodes), int(max_nodes), int(max_seqlen), _ptr(seq_lens), _ptr(block_tables), _ptr(cu_nodes), _ptr(node_pos),
-             _ptr(node_mask), _ptr(key_pos), None if axis is None else ctypes.addressof(axis), int(q_stride), int(node_stride))
+             _ptr(node_mask), _ptr(key_pos), None if axis is None else ctypes.addressof(axis), int(q_stride), int(node_stride),
+             int(total_tokens))
     t.kept = axis  # the host array lives as long as the struct
     return t
 

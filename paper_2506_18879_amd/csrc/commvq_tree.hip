@@ -39,6 +39,7 @@ struct TreeArgs {
     int block_bits, n_blocks, max_blocks;
     int total_nodes, max_nodes, max_seqlen;
     int splits, split_len, row_tiles;
+    int halves;                       // parts of a range of split_len tokens
     int turn;                         // 0: position_free, nothing is turned
     int q_bf16, cb_bf16;
     float scale2;                     // softmax scale times log2(e)
@@ -56,7 +57,12 @@ __device__ __forceinline__ Span span_of(const TreeArgs &a, int b)
     s.n = min(min(max(a.cu[b + 1], s.n0), a.total_nodes) - s.n0, a.max_nodes);
     return s;
 }
-__device__ __forceinline__ int axis_of(const TreeArgs &a, int j) { return (int)(a.axes[j >> 4] >> (2 * (j & 15))) & 3; }
+__device__ __forceinline__ int axis_of(const TreeArgs &a, int j)
+{
+    // (no indexing by lane: the words would be put into memory, or LDS, for it)
+    const unsigned w = j & 32 ? (j & 16 ? a.axes[3] : a.axes[2]) : (j & 16 ? a.axes[1] : a.axes[0]);
+    return (int)(w >> (2 * (j & 15))) & 3;
+}
 
 // E(m) of sub-space j, conjugated where `back` says so: a vector z turned by R_m is z conj E(m)
 __device__ __forceinline__ float2 turned_by(const TreeArgs &a, int m, int j)
@@ -184,10 +190,12 @@ __global__ __launch_bounds__(64 * NR) void k_tree_rows(const TreeArgs a)
         // the sums of the two tokens at first + 2 pair, first the first one's
         auto decode = [&](const uint8_t *pages, int M, const __amdgpu_buffer_rsrc_t rows, int i) {
             floatx4_t acc = {0.f, 0.f, 0.f, 0.f};
-            const int pa = __builtin_amdgcn_readlane(page, i), pb = __builtin_amdgcn_readlane(page, i + 1);
+            // (a token that does not count takes the other one's codes: its pieces meet that token's in a matrix instruction, times zero)
+            const int ia = seen >> i & 1u ? i : i + 1, ib = seen >> (i + 1) & 1u ? i + 1 : i;
+            const int pa = __builtin_amdgcn_readlane(page, ia), pb = __builtin_amdgcn_readlane(page, ib);
             const int in_page = (1 << a.block_bits) - 1;
-            const uint8_t *ca = pages + ((((size_t)pa * a.Hkv + g) << a.block_bits) + ((c0 + i) & in_page)) * M + 4 * gk;
-            const uint8_t *cb = pages + ((((size_t)pb * a.Hkv + g) << a.block_bits) + ((c0 + i + 1) & in_page)) * M + 4 * gk;
+            const uint8_t *ca = pages + ((((size_t)pa * a.Hkv + g) << a.block_bits) + ((c0 + ia) & in_page)) * M + 4 * gk;
+            const uint8_t *cb = pages + ((((size_t)pb * a.Hkv + g) << a.block_bits) + ((c0 + ib) & in_page)) * M + 4 * gk;
             for (int blk = 0; blk < M; blk += 16) {
                 const unsigned wa = *reinterpret_cast<const unsigned *>(ca + blk), wb = *reinterpret_cast<const unsigned *>(cb + blk);
                 uint4_t va[4], vb[4];
@@ -423,6 +431,13 @@ __global__ __launch_bounds__(256) void k_tree_rows_f32(const TreeArgs a)
     if (gk == 0) a.stat[row] = make_float2(m, l);
 }
 
+}  // namespace
+
+#include "commvq_tree_dense.hpp"
+#include "commvq_tree_stream.hpp"
+
+namespace {
+
 // ------------------------------------------------------------------ k_tree_final
 constexpr int kFinalWaves = 4;
 
@@ -450,7 +465,7 @@ __global__ __launch_bounds__(64 * kFinalWaves) void k_tree_final(const TreeArgs 
         const Span s = span_of(a, b);
         const int i = node - s.n0;
         if (i >= 0 && i < s.n) {
-            const int ns = (s.L + a.split_len - 1) / a.split_len;
+            const int ns = min((s.L + a.split_len - 1) / a.split_len * a.halves, a.splits);
             const size_t row = (size_t)blockIdx.x * a.splits;
             for (int k = wave; k < ns; k += kFinalWaves) {
                 const float2 st = a.stat[row + k];
@@ -525,16 +540,27 @@ __global__ __launch_bounds__(256) void k_tree_pack(const uint4 *__restrict__ cb,
 
 // ------------------------------------------------------------------ host side
 struct TreePlan {
-    int nr, rg;          // wavefronts and row tiles per wavefront of a workgroup
+    int nr, rg;          // rows gathered: wavefronts and row tiles of a wavefront; decoded ahead: wavefronts of different rows
     int row_tiles, splits, split_len;
-    size_t stat_at, bytes;
+    int tiles_per_head;  // decoded ahead: row tiles of 16 of all sequences
+    int pass_tiles, passes;  // decoded ahead: token tiles of a pass
+    size_t stat_at, q_at, keys_at, vals_at, seen_at, phases_at, bytes;
 };
 
 inline bool wide(const commvq_config &c) { return c.q_dtype != COMMVQ_BF16 || c.codebook_dtype != COMMVQ_BF16; }
 
+void tree_room(const commvq_handle *h, int batch, int total_nodes, bool stream, TreePlan &p)
+{
+    const size_t parts = (size_t)total_nodes * h->cfg.n_q_heads * p.splits;
+    p.stat_at = align_up(parts * kD * 4, 256);
+    p.q_at = align_up(p.stat_at + parts * 8, 256);
+    p.tiles_per_head = first_tile(total_nodes, h->G, batch) + 1;
+    p.bytes = std::max<size_t>(256, stream ? p.q_at + (size_t)p.tiles_per_head * h->cfg.n_kv_heads * 4096 : p.q_at);
+}
+
 // Rows of a workgroup: the smallest of 16, 32, 64, 128 and 256 that holds the largest tree's.  Ranges: as many as fill the chip with 16 wavefronts a
 // compute unit, in whole chunks.
-TreePlan tree_plan(const commvq_handle *h, int batch, int total_nodes, int max_nodes, int max_seqlen)
+TreePlan rows_plan(const commvq_handle *h, int batch, int total_nodes, int max_nodes, int max_seqlen)
 {
     TreePlan p{};
     const int rows = max_nodes * h->G;
@@ -549,10 +575,66 @@ TreePlan tree_plan(const commvq_handle *h, int batch, int total_nodes, int max_n
     const int64_t per = std::max<int64_t>(1, (chunks + want - 1) / want);
     p.split_len = (int)per * chunk;
     p.splits = (int)((chunks + per - 1) / per);
-    const size_t parts = (size_t)total_nodes * h->cfg.n_q_heads * p.splits;
-    p.stat_at = align_up(parts * kD * 4, 256);
-    p.bytes = std::max<size_t>(256, align_up(p.stat_at + parts * 8, 256));
+    tree_room(h, batch, total_nodes, false, p);
     return p;
+}
+
+// Ranges of k_tree_stream: whole tiles, so many a workgroup that the last round of workgroups (one per compute unit) ends soonest.
+TreePlan stream_plan(const commvq_handle *h, int batch, int total_nodes, int max_seqlen)
+{
+    TreePlan p{};
+    p.row_tiles = 1;
+    const int64_t units = (int64_t)batch * h->cfg.n_kv_heads, tiles = (max_seqlen + kStreamTile - 1) / kStreamTile;
+    double best = 0;
+    int64_t per = 1;
+    for (int64_t x = 1; x <= tiles; ++x) {
+        const double cost = (double)((units * ((tiles + x - 1) / x) + 255) / 256) * (x + 0.1);   // (a tenth of a tile for a workgroup's beginning)
+        if (x == 1 || cost < best) { best = cost; per = x; }
+    }
+    p.split_len = (int)per * kStreamTile;
+    p.splits = (int)((tiles + per - 1) / per);
+    tree_room(h, batch, total_nodes, false, p);
+    return p;
+}
+
+// Decoded ahead: passes over as many tiles as the scratch holds, which is 128 (tile, head)s, 128 MiB: what the 256 MiB behind the L2s hold from
+// one kernel to the next (decoding 128K tokens of 8 heads: 161 us in four such passes, 252 in two of twice the size, 217 in one).
+constexpr int kDenseTileHeads = 128;
+TreePlan dense_plan(const commvq_handle *h, int batch, int total_nodes, int max_nodes, int max_seqlen)
+{
+    TreePlan p{};
+    const int rows = max_nodes * h->G, groups = (rows + 16 * kDenseRows - 1) / (16 * kDenseRows), Hkv = h->cfg.n_kv_heads;
+    p.nr = groups <= 1 ? 1 : groups <= 2 ? 2 : groups <= 4 ? 4 : 8;
+    p.row_tiles = (groups + p.nr - 1) / p.nr;
+    const int tiles = (max_seqlen + kDecodeTile - 1) / kDecodeTile;
+    const int64_t all = (int64_t)batch * tiles;
+    p.pass_tiles = (int)std::min<int64_t>(all, std::max(1, kDenseTileHeads / Hkv));
+    p.passes = (int)((all + p.pass_tiles - 1) / p.pass_tiles);
+    p.split_len = kDecodeTile;
+    p.splits = std::min(tiles, p.pass_tiles) * kDenseHalves;
+    tree_room(h, batch, total_nodes, true, p);
+    const size_t steps = (size_t)p.pass_tiles * Hkv * kDecodeSteps;
+    p.keys_at = align_up(p.bytes, 256);
+    p.vals_at = p.keys_at + steps * kStepBytes;
+    p.seen_at = p.vals_at + steps * kStepBytes;
+    p.phases_at = align_up(p.seen_at + steps * 4, 256);
+    p.bytes = p.phases_at + (size_t)p.pass_tiles * kDecodeSteps * 16 * 64 * 16;
+    return p;
+}
+
+// Which kernels a call takes.  (What the workspace is sized for does not depend on tables and positions, which are not known then.)
+enum Way { kRows, kStream, kDense };
+Way tree_way(const commvq_handle *h, int batch, int max_nodes, int max_seqlen, bool tables, bool implicit)
+{
+    if (wide(h->cfg) || !tables || max_seqlen < 1) return kRows;
+    if ((int64_t)batch * h->cfg.n_kv_heads * ((max_seqlen + 1023) / 1024) < 96) return kRows;
+    return max_nodes * h->G <= kStreamRows && implicit ? kStream : kDense;
+}
+
+TreePlan plan_of(Way way, const commvq_handle *h, int batch, int total_nodes, int max_nodes, int max_seqlen)
+{
+    return way == kStream ? stream_plan(h, batch, total_nodes, max_seqlen) : way == kDense ? dense_plan(h, batch, total_nodes, max_nodes, max_seqlen)
+                                                                           : rows_plan(h, batch, total_nodes, max_nodes, max_seqlen);
 }
 
 commvq_status check_tree_sizes(const commvq_handle *h, int32_t batch, int32_t total_nodes, int32_t max_nodes, int32_t max_seqlen)
@@ -580,6 +662,77 @@ hipError_t launch_wide(const TreeArgs &a, dim3 grid, hipStream_t s)
     return hipGetLastError();
 }
 
+template <int NBK, int NBV>
+hipError_t launch_stream_as(const TreeArgs &a, const char *tables, dim3 grid, hipStream_t s)
+{
+    static std::atomic<uint64_t> lds_ok{0};
+    const hipError_t e = allow_dynamic_lds(k_tree_stream<NBK, NBV>, kTreeLds, lds_ok);
+    if (e != hipSuccess) return e;
+    k_tree_stream<NBK, NBV><<<grid, kStreamThreads, kTreeLds, s>>>(a, tables);
+    return hipGetLastError();
+}
+
+hipError_t launch_stream(const TreeArgs &a, const char *tables, dim3 grid, hipStream_t s)
+{
+    if (a.Mk == 16) return a.Mv == 16 ? launch_stream_as<1, 1>(a, tables, grid, s) : launch_stream_as<1, 2>(a, tables, grid, s);
+    return a.Mv == 16 ? launch_stream_as<2, 1>(a, tables, grid, s) : launch_stream_as<2, 2>(a, tables, grid, s);
+}
+
+bool explicit_positions(const TreeArgs &a) { return a.turn && (a.key_pos || a.n_axes > 1); }
+
+template <int NBK, int NBV>
+hipError_t launch_decode(const TreeArgs &a, const DensePass &d, const char *tables, dim3 grid, hipStream_t s)
+{
+    static std::atomic<uint64_t> ok0{0}, ok1{0};
+    if (explicit_positions(a)) {
+        const hipError_t e = allow_dynamic_lds(k_tree_decode<NBK, NBV, true>, kDecodeLds, ok1);
+        if (e != hipSuccess) return e;
+        k_tree_decode<NBK, NBV, true><<<grid, kDecodeThreads, kDecodeLds, s>>>(a, d, tables);
+    } else {
+        const hipError_t e = allow_dynamic_lds(k_tree_decode<NBK, NBV, false>, kDecodeLds, ok0);
+        if (e != hipSuccess) return e;
+        k_tree_decode<NBK, NBV, false><<<grid, kDecodeThreads, kDecodeLds, s>>>(a, d, tables);
+    }
+    return hipGetLastError();
+}
+
+template <int WR>
+hipError_t launch_dense_as(const TreeArgs &a, const DensePass &d, dim3 grid, hipStream_t s)
+{
+    static std::atomic<uint64_t> lds_ok{0};
+    const hipError_t e = allow_dynamic_lds(k_tree_dense<WR>, dense_lds(WR), lds_ok);
+    if (e != hipSuccess) return e;
+    k_tree_dense<WR><<<grid, 64 * kDenseWaves, dense_lds(WR), s>>>(a, d);
+    return hipGetLastError();
+}
+
+hipError_t launch_dense(const TreeArgs &a, const TreePlan &p, int passes, const char *tables, char *workspace, hipStream_t s)
+{
+    DensePass d{workspace + p.keys_at, workspace + p.vals_at, reinterpret_cast<unsigned *>(workspace + p.seen_at),
+                reinterpret_cast<floatx4_t *>(workspace + p.phases_at), reinterpret_cast<uint4_t *>(workspace + p.q_at),
+                p.tiles_per_head, 0, p.pass_tiles, 0, (a.max_nodes * a.G + 15) / 16};
+    const int64_t turns = ((int64_t)a.batch * a.Hkv * d.turn_tiles + kDecodeWaves - 1) / kDecodeWaves;
+    const int64_t decode = 2ll * d.tiles * a.Hkv, dense = (int64_t)d.tiles * a.Hkv * p.row_tiles * kDenseHalves;
+    if (std::max(turns + decode, dense) > 0x7fffffff) return hipErrorInvalidValue;
+    for (int i = 0; i < passes; ++i, d.tile0 += d.tiles) {
+        d.turn_wgs = i == 0 ? (int)turns : 0;
+        const dim3 first((unsigned)(d.turn_wgs + decode)), second((unsigned)dense);
+        hipError_t e;
+        if (explicit_positions(a)) {
+            k_tree_phases<<<dim3((unsigned)d.tiles * kDecodeSteps), 256, 0, s>>>(a, d);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        if (a.Mk == 16) e = a.Mv == 16 ? launch_decode<1, 1>(a, d, tables, first, s) : launch_decode<1, 2>(a, d, tables, first, s);
+        else e = a.Mv == 16 ? launch_decode<2, 1>(a, d, tables, first, s) : launch_decode<2, 2>(a, d, tables, first, s);
+        if (e != hipSuccess) return e;
+        e = p.nr == 1 ? launch_dense_as<1>(a, d, second, s) : p.nr == 2 ? launch_dense_as<2>(a, d, second, s) : p.nr == 4 ? launch_dense_as<4>(a, d, second, s)
+                                                                                                          : launch_dense_as<8>(a, d, second, s);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 bool misaligned(std::initializer_list<const void *> ps)
 {
     uintptr_t all = 0;
@@ -597,7 +750,10 @@ commvq_status commvq_tree_workspace_bytes(const commvq_handle *h, int32_t batch,
     if (!h || !bytes) return COMMVQ_ERR_NULL;
     const commvq_status st = check_tree_sizes(h, batch, total_nodes, max_nodes, max_seqlen);
     if (st != COMMVQ_OK) return st;
-    *bytes = tree_plan(h, batch, total_nodes, max_nodes, max_seqlen).bytes;
+    *bytes = 0;
+    for (const bool tables : {false, true})
+        for (const bool implicit : {false, true})
+            *bytes = std::max(*bytes, plan_of(tree_way(h, batch, max_nodes, max_seqlen, tables, implicit), h, batch, total_nodes, max_nodes, max_seqlen).bytes);
     return COMMVQ_OK;
 }
 
@@ -618,6 +774,7 @@ commvq_status commvq_tree_attn(commvq_handle *h, const commvq_pages *pages, cons
     if ((int64_t)t->max_seqlen > (int64_t)pages->max_blocks * pages->block_size) return COMMVQ_ERR_SHAPE;
     // keys at positions 0 .. L - 1 and nodes at or after the last of them
     if (!t->key_pos && !c.position_free && (int64_t)t->max_seqlen - 1 > c.max_position) return COMMVQ_ERR_SHAPE;
+    if (t->total_tokens && (t->total_tokens < t->max_seqlen || t->total_tokens > (int64_t)t->batch * t->max_seqlen)) return COMMVQ_ERR_SHAPE;
     if (misaligned({q, node_keys, node_vals, key_pages, val_pages, key_cb, val_cb, tables, out})) return COMMVQ_ERR_SHAPE;
     const int64_t q_row = (int64_t)c.n_q_heads * kD, node_row = (int64_t)c.n_kv_heads * kD;
     if (t->q_stride && (t->q_stride < q_row || t->q_stride % 8)) return COMMVQ_ERR_SHAPE;
@@ -628,10 +785,16 @@ commvq_status commvq_tree_attn(commvq_handle *h, const commvq_pages *pages, cons
             if (t->pair_axis[j] >= pages->n_axes) return COMMVQ_ERR_SHAPE;
             a.axes[j >> 4] |= (unsigned)t->pair_axis[j] << (2 * (j & 15));
         }
-    const TreePlan p = tree_plan(h, t->batch, t->total_nodes, t->max_nodes, t->max_seqlen);
+    size_t need = 0;
+    st = commvq_tree_workspace_bytes(h, t->batch, t->total_nodes, t->max_nodes, t->max_seqlen, &need);
+    if (st != COMMVQ_OK) return st;
+    const Way way = tree_way(h, t->batch, t->max_nodes, t->max_seqlen, tables != nullptr, pages->n_axes == 1 && !t->key_pos);
+    const TreePlan p = plan_of(way, h, t->batch, t->total_nodes, t->max_nodes, t->max_seqlen);
+    // (what the device may hold of it beyond this is left out: whole tiles, sequence by sequence)
+    const int64_t tiles = t->total_tokens ? std::min<int64_t>((int64_t)p.pass_tiles * p.passes, t->total_tokens / kDecodeTile + t->batch) : (int64_t)p.pass_tiles * p.passes;
     const int64_t wgs = (int64_t)t->batch * c.n_kv_heads * p.row_tiles * p.splits;
     if (wgs > 0x7fffffff) return COMMVQ_ERR_SHAPE;
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < p.bytes) return COMMVQ_ERR_WORKSPACE;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < need) return COMMVQ_ERR_WORKSPACE;
     if (h->device < 0) return COMMVQ_ERR_NO_DEVICE;
     int dev = -1;
     if (hipGetDevice(&dev) != hipSuccess || dev != h->device) return COMMVQ_ERR_NO_DEVICE;  // the phase tables are another GPU's
@@ -646,14 +809,16 @@ commvq_status commvq_tree_attn(commvq_handle *h, const commvq_pages *pages, cons
     a.batch = t->batch; a.Hq = c.n_q_heads; a.Hkv = c.n_kv_heads; a.G = h->G; a.Mk = c.m_key; a.Mv = c.m_val; a.n_hi = h->n_hi;
     a.n_axes = pages->n_axes; a.block_bits = __builtin_ctz((unsigned)pages->block_size); a.n_blocks = pages->n_blocks; a.max_blocks = pages->max_blocks;
     a.total_nodes = t->total_nodes; a.max_nodes = t->max_nodes; a.max_seqlen = t->max_seqlen;
-    a.splits = p.splits; a.split_len = p.split_len; a.row_tiles = p.row_tiles;
+    a.splits = p.splits; a.split_len = p.split_len; a.row_tiles = p.row_tiles; a.halves = way == kDense ? kDenseHalves : 1;
     a.turn = !c.position_free; a.q_bf16 = c.q_dtype == COMMVQ_BF16; a.cb_bf16 = c.codebook_dtype == COMMVQ_BF16;
     a.scale2 = h->scale * kLog2e;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (wgs > 0) {
         const dim3 grid((unsigned)wgs);
         hipError_t e;
-        if (wide(c)) e = launch_wide(a, grid, s);
+        if (way == kDense) e = launch_dense(a, p, (int)((tiles + p.pass_tiles - 1) / p.pass_tiles), static_cast<const char *>(tables), static_cast<char *>(workspace), s);
+        else if (way == kStream) e = launch_stream(a, static_cast<const char *>(tables), grid, s);
+        else if (wide(c)) e = launch_wide(a, grid, s);
         else if (p.nr == 1) e = launch_rows<1, 1>(a, grid, s);
         else if (p.nr == 2) e = launch_rows<2, 1>(a, grid, s);
         else if (p.nr == 4) e = launch_rows<4, 1>(a, grid, s);

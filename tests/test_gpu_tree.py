@@ -57,6 +57,7 @@ class Case:
         self.node_pos = torch.tensor(node_pos, dtype=torch.int32).view(-1, axes)
         self.tables_wanted = tables and q == cb == "bf16"
         self.q_stride = self.node_stride = 0
+        self.more = {}
 
     def call(self, handle=None, mask="own", total=None, max_len=None):
         h = handle or cv.commvq_create(self.cfg)
@@ -69,7 +70,7 @@ class Case:
         total, max_len = total or self.N, max(self.lens) if max_len is None else max_len
         pages = cv.make_pages(self.block, self.pool, self.width, self.axes)
         tree = cv.make_tree(self.B, total, max(self.nodes), max_len, self.d["lens"], self.d["table"], self.d["cu"], self.d["pos"],
-                            self.d["mask"] if mask == "own" else None, self.key_pos, _axis_map(self.axes) if self.axes > 1 else None, self.q_stride, self.node_stride)
+                            self.d["mask"] if mask == "own" else None, self.key_pos, _axis_map(self.axes) if self.axes > 1 else None, self.q_stride, self.node_stride, **self.more)
         tables = None
         if self.tables_wanted:
             tables = torch.empty(cv.commvq_tree_table_bytes(h), dtype=torch.uint8, device="cuda")
@@ -140,10 +141,12 @@ class Case:
         err = (got - want).abs()
         norm = float((got - want).norm() / want.norm().clamp(min=1e-300)) if float(want.norm()) else float(err.max())
         if self.out.dtype == torch.bfloat16:
-            assert bool((err <= ((2 * d).exp() * (1 + U) ** 3 - 1) * mass + U * want.abs()).all()), float((err / mass.clamp(min=1e-30)).max())
+            fits = bool((err <= ((2 * d).exp() * (1 + U) ** 3 - 1) * mass + U * want.abs()).all())
+            assert fits, float((err / mass.clamp(min=1e-30)).max())
             assert norm <= 2 * 1.29 * U, norm
         else:
-            assert bool((err <= 4 * 1.2e-5 * mass + 1e-30).all()), float((err / mass.clamp(min=1e-30)).max())
+            fits = bool((err <= 4 * 1.2e-5 * mass + 1e-30).all())
+            assert fits, float((err / mass.clamp(min=1e-30)).max())
             assert norm <= 1.2e-5, norm
 
 
@@ -263,7 +266,7 @@ def test_what_masked_nodes_hold_does_not_matter():
     assert not torch.isfinite(c.out[i]).any() and not torch.isfinite(c.out[10]).any()
 
 
-@pytest.mark.parametrize("n", [70, 1500, 5000])
+@pytest.mark.parametrize("n", [70, 77, 1500, 5001])
 def test_codewords_that_no_counted_token_selects(n):
     # tails of pages, pages that are not there and rows past the context select infinities; no weight may touch them
     c = Case([n], [tree(5)], Hkv=1, seed=n, spare=1)
@@ -321,7 +324,8 @@ def test_large_logits():
     c.q *= 30
     c.call()
     want, mass, d = c.plain()
-    assert bool(((c.out.double() - want).abs() <= ((2 * d).exp() * (1 + U) ** 3 - 1) * mass + U * want.abs()).all())
+    fits = bool(((c.out.double() - want).abs() <= ((2 * d).exp() * (1 + U) ** 3 - 1) * mass + U * want.abs()).all())
+    assert fits
 
 
 def test_the_same_bits_from_call_to_call_and_on_another_stream():
@@ -384,6 +388,126 @@ def test_single_nodes_agree_with_decode_attention_of_the_flat_cache():
     c.check()
     assert float((c.out.double() - flat.double()).norm() / flat.double().norm()) <= 2 * 1.29 * U
     op.close()
+
+
+# ---- contexts long enough for the kernels that stream whole codebooks (up to 16 rows a KV head: in one go; more: decoded ahead, in passes)
+@pytest.mark.parametrize("k,G", [(1, 1), (1, 8), (4, 4), (2, 8), (5, 4), (33, 1), (9, 8), (17, 8), (35, 8)])
+def test_long_rows(k, G):
+    c = Case([12300], [tree(k)], Hkv=8, G=G, seed=100 + k + G)
+    c.call()
+    c.check()
+
+
+@pytest.mark.parametrize("k", [3, 20])
+@pytest.mark.parametrize("Mk,Mv", [(32, 16), (16, 32), (32, 32)])
+def test_long_codebooks(Mk, Mv, k):
+    c = Case([12289], [tree(k)], Hkv=8, G=4, Mk=Mk, Mv=Mv, seed=Mk + Mv + k)
+    c.call()
+    c.check()
+
+
+@pytest.mark.parametrize("most", [4, 12])
+@pytest.mark.parametrize("block", [16, 1024])
+def test_long_ragged(most, block):
+    import random
+    r = random.Random(most + block)
+    lens = [0, 1, 2047, 2048, 2049, 4096, 4097, 0, 6143] + [r.randrange(5000) for _ in range(70)]
+    ks = [r.randrange(0, most + 1) for _ in lens]
+    ks[3] = most
+    for sizes in ({}, {"total_tokens": sum(lens)}):
+        c = Case(lens, [tree(k, i) for i, k in enumerate(ks)], Hkv=2, G=4, block=block, seed=most + block)
+        c.more = sizes
+        c.call()
+        c.check()
+
+
+@pytest.mark.parametrize("k", [4, 10, 40])
+def test_long_sequences_over_several_passes(k):
+    # 16 tiles of 2048 tokens a pass for 8 heads: the first and the last sequence are in several
+    c = Case([70001, 3000, 40000], [tree(k), tree(2), tree(min(3, k))], Hkv=8, G=1 if k == 40 else 2, block=64, max_position=1 << 17, seed=k)
+    c.call()
+    c.check()
+
+
+@pytest.mark.parametrize("axes", [1, 3])
+@pytest.mark.parametrize("k", [2, 30])
+def test_long_explicit_positions(k, axes):
+    where = lambda gen, n, a: torch.randint(-9000, 30000, (n, a), generator=gen, device="cuda", dtype=torch.int32)
+    c = Case([13000], [tree(k)], Hkv=8, G=4, axes=axes, key_pos=where, node_pos=[[4000 + i + 50 * a for a in range(axes)] for i in range(k)], seed=k + axes)
+    c.call()
+    c.check()
+
+
+@pytest.mark.parametrize("k", [3, 18])
+@pytest.mark.parametrize("how", ["axes without stored positions", "far", "before the context", "position free"])
+def test_long_positions(how, k):
+    kw = {"axes without stored positions": dict(axes=2), "far": {}, "before the context": dict(node_pos=[[i - 500] for i in range(k)]), "position free": dict(position_free=True)}[how]
+    if how == "far":
+        top = 2 ** 31 - 1 - 20000
+        kw = dict(key_pos=lambda gen, n, a: top + torch.randint(0, 14000, (n, a), generator=gen, device="cuda", dtype=torch.int32), node_pos=[[top + 14000 + i] for i in range(k)])
+    c = Case([12500], [tree(k)], Hkv=8, G=4, seed=k, **kw)
+    c.call()
+    c.check()
+
+
+@pytest.mark.parametrize("k", [3, 18])
+def test_long_codewords_that_no_counted_token_selects(k):
+    c = Case([13001, 20], [tree(k), tree(2)], Hkv=8, seed=k, spare=1)
+    c.key_cb[:, :, 0], c.val_cb[:, :, 0] = float("nan"), float("inf")
+    c.key_pages.clamp_(min=1)
+    c.val_pages.clamp_(min=1)
+    last = int(c.table[0, 13000 // 16])
+    c.key_pages[last, :, 13001 % 16:], c.val_pages[last, :, 13001 % 16:] = 0, 0
+    c.key_pages[0], c.val_pages[0] = 0, 0
+    c.table[0][c.table[0] == 0] = -1
+    c.table[0, 1], c.table[0, 300], c.table[0, 500:640] = c.pool, 2 ** 31 - 1, -5
+    c.call()
+    c.check()
+
+
+@pytest.mark.parametrize("k", [3, 18])
+def test_long_contexts_without_a_single_page(k):
+    c = Case([12500, 700], [tree(k), tree(2)], Hkv=8, seed=k)
+    c.table[:] = -1
+    c.call()
+    c.check()
+
+
+@pytest.mark.parametrize("k", [4, 40])
+def test_long_captured_and_replayed(k):
+    c = Case([40000, 100], [tree(k), tree(3)], Hkv=8, G=2, block=64, max_position=1 << 16, seed=k)
+    h = cv.commvq_create(c.cfg)
+    want = c.call(handle=h).clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.again()
+    for i in range(4):
+        c.out.zero_()
+        c.kept[1].fill_(255 - i)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(want, c.out)
+        c.again()
+        torch.cuda.synchronize()
+        assert torch.equal(want, c.out)
+    c.d["lens"][0] = c.lens[0] = 30000
+    graph.replay()
+    torch.cuda.synchronize()
+    c.check()
+    cv.commvq_destroy(h)
+
+
+def test_codes_beyond_32_bit_offsets():
+    """Pages past 4 GiB of the pool, short and long contexts."""
+    for lens, k in (([500], 3), ([12400], 3), ([12400], 9)):
+        c = Case(lens, [tree(k)], Hkv=8, G=4, Mk=32, Mv=32, block=1024, spare=(9 << 29) // (1024 * 8 * 32) + 1, seed=k)
+        held = -(-lens[0] // 1024)
+        c.table[0, :held] = torch.arange(c.pool - held, c.pool, dtype=torch.int32)
+        assert c.key_pages.numel() > 1 << 32
+        c.call()
+        c.check()
+        del c
+        torch.cuda.empty_cache()
 
 
 def test_random_batches():
