@@ -106,17 +106,21 @@ __device__ __forceinline__ void selection(int lane, uint4_t &sel, unsigned &sidx
 }
 
 // ------------------------------------------------------------------ k_tree_rows
-// One range of a context for 16 NR RG rows of a KV head: NR wavefronts with RG tiles of 16 rows each share 32 decoded tokens at a time.
+// One range of a context for 16 NR RG rows of a KV head, 32 tokens at a time.  All eight wavefronts decode four tokens of them each; then NR
+// of them have RG tiles of 16 different rows, 8 / NR of them different elements of the same rows (whose logits each makes by itself).
 // Decode: the four 16-lane rows of a wavefront hold four codebooks, a lane a 16-byte piece of a codeword; two tokens' pieces
 // are the dense operand of v_smfmac_f32_16x16x64_bf16, whose constant 0/1 operand adds them in fp32 (exactly: products with 1.0).
 // A lane then has four elements of one token, turns them (keys), rounds them to bf16, as a cache of bf16 keys and values
 // would, and leaves them in LDS.  Products: K Q^T with tokens as rows, so that a lane has 4 tokens of one query row; what it
 // makes of them is, without any exchange, the operand of V^T P^T, whose other operand is read from LDS by columns.
-// Bound by the codeword rows' way through the L1s, 256 bytes a codebook and token; taken for contexts that the streamed kernel's 2 MiB of
-// codebooks per workgroup do not pay for.
+// Short contexts are bound by the chain pages -> codes -> rows, so codes are asked for a chunk ahead and a wavefront's rows all at once; longer
+// ones by the codeword rows' way through the L1s, 256 bytes a codebook and token.
+constexpr int kRowsWaves = 8;
+constexpr int kOwn = kChunk / kRowsWaves;       // tokens that a wavefront decodes of a chunk
 template <int NR, int RG, bool AXES>
-__global__ __launch_bounds__(64 * NR) void k_tree_rows(const TreeArgs a)
+__global__ __launch_bounds__(64 * kRowsWaves) void k_tree_rows(const TreeArgs a)
 {
+    constexpr int ND = kRowsWaves / NR, NX = 8 / ND;                 // wavefronts of a row tile; tiles of 16 elements of a wavefront
     __shared__ __align__(16) char ktile[kChunk * kRowBytes], vtile[kChunk * kRowBytes];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int id = blockIdx.x;
@@ -128,7 +132,33 @@ __global__ __launch_bounds__(64 * NR) void k_tree_rows(const TreeArgs a)
     const Span s = span_of(a, b);
     const int R = s.n * a.G, r0 = rt * 16 * NR * RG, t_begin = split * a.split_len, t_end = min(s.L, t_begin + a.split_len);
     if (r0 >= R || t_begin >= t_end) return;
-    const int n = lane & 15, gk = lane >> 4;
+    const int n = lane & 15, gk = lane >> 4, wr = wave / ND, wd = wave % ND;
+
+    // codes of the wavefront's tokens c0 + 4 wave .. + 3, a chunk ahead: lane row gk has books 4 gk .. + 3 of every block of 16
+    const int32_t *table = a.tables + (size_t)b * a.max_blocks;
+    const int in_page = (1 << a.block_bits) - 1;
+    unsigned seen_next = 0, ck_next[kOwn][2], cv_next[kOwn][2];
+    int slot_next = 0;                                               // of token c0 + lane % 32
+    auto ask = [&](int c0) __attribute__((always_inline)) {
+        const int tok = c0 + (lane & (kChunk - 1));
+        const int page = table[min(tok, t_end - 1) >> a.block_bits];
+        const bool there = tok < t_end && page >= 0 && page < a.n_blocks;
+        seen_next = (unsigned)__ballot(there);                       // (both halves of the wavefront hold the 32 tokens)
+        slot_next = ((there ? page : 0) << a.block_bits) + (tok & in_page);   // (any page does for a token that is not counted)
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            // (a token that does not count takes its neighbour's codes: its pieces meet that token's in a matrix instruction, times zero)
+            const int mine = wave * kOwn + i, from = seen_next >> mine & 1u ? mine : mine ^ 1;
+            const int slot = __builtin_amdgcn_readlane(slot_next, from);
+            const size_t rec = (((size_t)(slot >> a.block_bits) * a.Hkv + g) << a.block_bits) + (slot & in_page);
+            const unsigned *k = reinterpret_cast<const unsigned *>(a.key_pages + rec * a.Mk) + gk, *v = reinterpret_cast<const unsigned *>(a.val_pages + rec * a.Mv) + gk;
+            ck_next[i][0] = k[0];
+            cv_next[i][0] = v[0];
+            ck_next[i][1] = a.Mk == 32 ? k[4] : 0u;
+            cv_next[i][1] = a.Mv == 32 ? v[4] : 0u;
+        }
+    };
+    ask(t_begin);
 
     int t0[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -140,7 +170,7 @@ __global__ __launch_bounds__(64 * NR) void k_tree_rows(const TreeArgs a)
     uint4_t qv[RG][4];
 #pragma unroll
     for (int rg = 0; rg < RG; ++rg) {
-        const int r = r0 + (wave * RG + rg) * 16 + n;
+        const int r = r0 + (wr * RG + rg) * 16 + n;
         const int node = r / a.G, h = r % a.G;
         const bool there = r < R;
         const size_t at = (size_t)(s.n0 + (there ? node : 0)) * a.q_stride + (size_t)(g * a.G + h) * kD;
@@ -168,73 +198,79 @@ __global__ __launch_bounds__(64 * NR) void k_tree_rows(const TreeArgs a)
     const __amdgpu_buffer_rsrc_t krows = make_rsrc(static_cast<const uint16_t *>(a.key_cb) + (size_t)g * a.Mk * kK * kD, (unsigned)(a.Mk * kK * kD * 2));
     const __amdgpu_buffer_rsrc_t vrows = make_rsrc(static_cast<const uint16_t *>(a.val_cb) + (size_t)g * a.Mv * kK * kD, (unsigned)(a.Mv * kK * kD * 2));
     const unsigned lane_at = (unsigned)(4 * gk) * (kK * kD * 2) + (unsigned)n * 16u;
-    const int32_t *table = a.tables + (size_t)b * a.max_blocks;
 
-    floatx4_t o[RG][8];                              // element 16 x + 4 gk + i of row n
+    floatx4_t o[RG][NX];                             // element 16 (wd NX + x) + 4 gk + i of row n
     float m[RG], l[RG];
 #pragma unroll
     for (int rg = 0; rg < RG; ++rg) {
         m[rg] = -INFINITY;
         l[rg] = 0.f;
 #pragma unroll
-        for (int x = 0; x < 8; ++x) o[rg][x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+        for (int x = 0; x < NX; ++x) o[rg][x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
     }
+    // the sums of two tokens, by 16 codebooks
+    auto fetch = [&](const __amdgpu_buffer_rsrc_t rows, unsigned code, int blk, uint4_t (&v)[4]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int st = 0; st < 4; ++st)
+            v[st] = __builtin_amdgcn_raw_buffer_load_b128(rows, lane_at + ((code >> (8 * st) & 255u) << 8), (16 * blk + st) * (kK * kD * 2), 0);
+    };
+    auto add = [&](floatx4_t acc, const uint4_t (&va)[4], const uint4_t (&vb)[4]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int st = 0; st < 4; ++st) {
+            const uint8v_t both = {va[st][0], va[st][1], va[st][2], va[st][3], vb[st][0], vb[st][1], vb[st][2], vb[st][3]};
+            acc = __builtin_amdgcn_smfmac_f32_16x16x64_bf16(selv, __builtin_bit_cast(bf16x16_t, both), acc, (int)sidx, 0, 0);
+        }
+        return acc;
+    };
+    auto decode = [&](const __amdgpu_buffer_rsrc_t rows, const unsigned (&c)[kOwn][2], int M, floatx4_t (&acc)[kOwn / 2]) __attribute__((always_inline)) {
+        uint4_t v[kOwn][4];
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) fetch(rows, c[i][0], 0, v[i]);
+#pragma unroll
+        for (int p = 0; p < kOwn / 2; ++p) acc[p] = add(floatx4_t{0.f, 0.f, 0.f, 0.f}, v[2 * p], v[2 * p + 1]);
+        if (M == 32) {
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) fetch(rows, c[i][1], 1, v[i]);
+#pragma unroll
+            for (int p = 0; p < kOwn / 2; ++p) acc[p] = add(acc[p], v[2 * p], v[2 * p + 1]);
+        }
+    };
 
-    constexpr int PER = kChunk / NR;                 // tokens that a wavefront decodes
     for (int c0 = t_begin; c0 < t_end; c0 += kChunk) {
-        const int tok = c0 + (lane & (kChunk - 1));
-        int page = tok < t_end ? table[tok >> a.block_bits] : -1;
-        const bool there = page >= 0 && page < a.n_blocks;
-        const unsigned seen = (unsigned)__ballot(there);   // (both halves of the wavefront hold the 32 tokens)
-        page = there ? page : 0;                     // any page does for a token that is not counted
-        // the sums of the two tokens at first + 2 pair, first the first one's
-        auto decode = [&](const uint8_t *pages, int M, const __amdgpu_buffer_rsrc_t rows, int i) {
-            floatx4_t acc = {0.f, 0.f, 0.f, 0.f};
-            // (a token that does not count takes the other one's codes: its pieces meet that token's in a matrix instruction, times zero)
-            const int ia = seen >> i & 1u ? i : i + 1, ib = seen >> (i + 1) & 1u ? i + 1 : i;
-            const int pa = __builtin_amdgcn_readlane(page, ia), pb = __builtin_amdgcn_readlane(page, ib);
-            const int in_page = (1 << a.block_bits) - 1;
-            const uint8_t *ca = pages + ((((size_t)pa * a.Hkv + g) << a.block_bits) + ((c0 + ia) & in_page)) * M + 4 * gk;
-            const uint8_t *cb = pages + ((((size_t)pb * a.Hkv + g) << a.block_bits) + ((c0 + ib) & in_page)) * M + 4 * gk;
-            for (int blk = 0; blk < M; blk += 16) {
-                const unsigned wa = *reinterpret_cast<const unsigned *>(ca + blk), wb = *reinterpret_cast<const unsigned *>(cb + blk);
-                uint4_t va[4], vb[4];
+        unsigned ck[kOwn][2], cv[kOwn][2];
+        const unsigned seen = seen_next;
+        const int slot = slot_next;
 #pragma unroll
-                for (int st = 0; st < 4; ++st) {
-                    const int row = (blk + st) * (kK * kD * 2);
-                    va[st] = __builtin_amdgcn_raw_buffer_load_b128(rows, lane_at + ((wa >> (8 * st) & 255u) << 8), row, 0);
-                    vb[st] = __builtin_amdgcn_raw_buffer_load_b128(rows, lane_at + ((wb >> (8 * st) & 255u) << 8), row, 0);
-                }
+        for (int i = 0; i < kOwn; ++i)
 #pragma unroll
-                for (int st = 0; st < 4; ++st) {
-                    const uint8v_t both = {va[st][0], va[st][1], va[st][2], va[st][3], vb[st][0], vb[st][1], vb[st][2], vb[st][3]};
-                    acc = __builtin_amdgcn_smfmac_f32_16x16x64_bf16(selv, __builtin_bit_cast(bf16x16_t, both), acc, (int)sidx, 0, 0);
-                }
-            }
-            return acc;
-        };
-#pragma unroll 2
-        for (int p = 0; p < PER; p += 2) {
-            const int i = wave * PER + p;
-            floatx4_t k = decode(a.key_pages, a.Mk, krows, i);
-            const int mine = i + second;
-            if (a.turn) {
-                const int j = 4 * n + 2 * half;
+            for (int k = 0; k < 2; ++k) { ck[i][k] = ck_next[i][k]; cv[i][k] = cv_next[i][k]; }
+        if (c0 + kChunk < t_end) ask(c0 + kChunk);
+        float2 e[kOwn / 2][2];
+#pragma unroll
+        for (int p = 0; p < kOwn / 2; ++p)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                e[p][u] = make_float2(1.f, 0.f);
+                if (!a.turn) continue;
+                const int mine = wave * kOwn + 2 * p + second, j = 4 * n + 2 * half + u, ax = AXES ? axis_of(a, j) : 0;
                 int pos = c0 + mine;
-                const int32_t *own = nullptr;
-                if (a.key_pos) {
-                    const int pg = second ? __builtin_amdgcn_readlane(page, i + 1) : __builtin_amdgcn_readlane(page, i);
-                    own = a.key_pos + (((size_t)pg << a.block_bits) + (pos & ((1 << a.block_bits) - 1))) * a.n_axes;
-                }
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int ax = AXES ? axis_of(a, j + u) : 0;
-                    const float2 z = times(make_float2(k[2 * u], k[2 * u + 1]), turned_by(a, (own ? own[ax] : pos) - origin(ax), j + u));
-                    k[2 * u] = z.x;
-                    k[2 * u + 1] = z.y;
-                }
+                if (a.key_pos) pos = a.key_pos[(size_t)__shfl(slot, mine) * a.n_axes + ax];
+                e[p][u] = turned_by(a, pos - origin(ax), j);
             }
-            *reinterpret_cast<uint2_t *>(ktile + mine * kRowBytes + n * 16 + half * 8) = uint2_t{pack_bf16(k[0], k[1]), pack_bf16(k[2], k[3])};
+        floatx4_t acc[kOwn / 2];
+        decode(krows, ck, a.Mk, acc);
+#pragma unroll
+        for (int p = 0; p < kOwn / 2; ++p) {
+            const float2 z0 = times(make_float2(acc[p][0], acc[p][1]), e[p][0]), z1 = times(make_float2(acc[p][2], acc[p][3]), e[p][1]);
+            *reinterpret_cast<uint2_t *>(ktile + (wave * kOwn + 2 * p + second) * kRowBytes + n * 16 + half * 8) = uint2_t{pack_bf16(z0.x, z0.y), pack_bf16(z1.x, z1.y)};
+        }
+        decode(vrows, cv, a.Mv, acc);
+#pragma unroll
+        for (int p = 0; p < kOwn / 2; ++p) {
+            const int mine = wave * kOwn + 2 * p + second;
+            const bool counts = seen >> mine & 1u;   // (a weight of zero does not hide an infinity)
+            *reinterpret_cast<uint2_t *>(vtile + mine * kRowBytes + n * 16 + half * 8) =
+                uint2_t{counts ? pack_bf16(acc[p][0], acc[p][1]) : 0u, counts ? pack_bf16(acc[p][2], acc[p][3]) : 0u};
         }
         __syncthreads();
         floatx4_t sc[RG][2];
@@ -249,14 +285,6 @@ __global__ __launch_bounds__(64 * NR) void k_tree_rows(const TreeArgs a)
                 for (int rg = 0; rg < RG; ++rg)
                     sc[rg][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kv), __builtin_bit_cast(bf16x8_t, qv[rg][ks]), sc[rg][t], 0, 0, 0);
             }
-#pragma unroll 2
-        for (int p = 0; p < PER; p += 2) {
-            const int i = wave * PER + p, mine = i + second;
-            const floatx4_t v = decode(a.val_pages, a.Mv, vrows, i);
-            const bool counts = seen >> mine & 1u;   // (a weight of zero does not hide an infinity)
-            *reinterpret_cast<uint2_t *>(vtile + mine * kRowBytes + n * 16 + half * 8) =
-                uint2_t{counts ? pack_bf16(v[0], v[1]) : 0u, counts ? pack_bf16(v[2], v[3]) : 0u};
-        }
         uint4_t pv[RG];
 #pragma unroll
         for (int rg = 0; rg < RG; ++rg) {
@@ -265,7 +293,7 @@ __global__ __launch_bounds__(64 * NR) void k_tree_rows(const TreeArgs a)
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if (!(seen >> (16 * t + 4 * gk + i) & 1u)) sc[rg][t][i] = -INFINITY;
+                    sc[rg][t][i] = seen >> (16 * t + 4 * gk + i) & 1u ? sc[rg][t][i] : -INFINITY;
                     top = fmaxf(top, sc[rg][t][i]);
                 }
             top = fmaxf(top, __shfl_xor(top, 16));
@@ -285,42 +313,44 @@ __global__ __launch_bounds__(64 * NR) void k_tree_rows(const TreeArgs a)
 #pragma unroll
             for (int i = 0; i < 4; ++i) pv[rg][i] = pack_bf16(w[2 * i], w[2 * i + 1]);
 #pragma unroll
-            for (int x = 0; x < 8; ++x) o[rg][x] *= old;
+            for (int x = 0; x < NX; ++x) o[rg][x] *= old;
         }
-        __syncthreads();
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-            const char *at = vtile + (4 * gk + n / 4) * kRowBytes + 32 * x + 8 * (n & 3);
+        for (int x = 0; x < NX; ++x) {
+            const char *at = vtile + (4 * gk + n / 4) * kRowBytes + 32 * (wd * NX + x) + 8 * (n & 3);
             const uint2_t v0 = lds_read_columns(at), v1 = lds_read_columns(at + 16 * kRowBytes);
             const uint4_t vv = {v0[0], v0[1], v1[0], v1[1]};
 #pragma unroll
             for (int rg = 0; rg < RG; ++rg)
                 o[rg][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vv), __builtin_bit_cast(bf16x8_t, pv[rg]), o[rg][x], 0, 0, 0);
         }
+        if (c0 + kChunk < t_end) __syncthreads();
     }
 #pragma unroll
     for (int rg = 0; rg < RG; ++rg) {
         float sum = l[rg];
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        const int r = r0 + (wave * RG + rg) * 16 + n;
+        const int r = r0 + (wr * RG + rg) * 16 + n;
         if (r >= R) continue;
         const size_t row = ((size_t)(s.n0 + r / a.G) * a.Hq + g * a.G + r % a.G) * a.splits + split;
 #pragma unroll
-        for (int x = 0; x < 8; ++x) *reinterpret_cast<floatx4_t *>(a.part + row * kD + 16 * x + 4 * gk) = o[rg][x];
-        if (gk == 0) a.stat[row] = make_float2(m[rg], sum);
+        for (int x = 0; x < NX; ++x) *reinterpret_cast<floatx4_t *>(a.part + row * kD + 16 * (wd * NX + x) + 4 * gk) = o[rg][x];
+        if (gk == 0 && wd == 0) a.stat[row] = make_float2(m[rg], sum);
     }
 }
 
 // ------------------------------------------------------------------ k_tree_rows_f32
 // The same in fp32 throughout, for fp32 queries or codebooks: four wavefronts with 16 rows each, 16 tokens at a time.  A thread decodes 8
-// elements of a token by vector additions; products by v_mfma_f32_16x16x4_f32, whose operands have one element a lane, so that
+// elements of a token by vector additions, keys first (32 fp32 codebooks of keys fill an L2; four wavefronts more for the values at the same time:
+// one head, 4096 tokens 23.9 -> 30.6 us); products by v_mfma_f32_16x16x4_f32, whose operands have one element a lane, so that
 // a weight is an operand of the second product as it is.
+constexpr int kWideThreads = 256;
 template <bool Q16, bool CB16>
-__global__ __launch_bounds__(256) void k_tree_rows_f32(const TreeArgs a)
+__global__ __launch_bounds__(kWideThreads) void k_tree_rows_f32(const TreeArgs a)
 {
     __shared__ __align__(16) float ktile[kWideChunk * kWideRow], vtile[kWideChunk * kWideRow];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int id = blockIdx.x;
     const int g = id % a.Hkv;
     id /= a.Hkv;
@@ -345,7 +375,7 @@ __global__ __launch_bounds__(256) void k_tree_rows_f32(const TreeArgs a)
         if (a.turn) z = times(z, turned_by(a, a.node_pos[(size_t)node * a.n_axes + ax] - a.node_pos[(size_t)s.n0 * a.n_axes + ax], j));
         qv[x] = row_there ? (e & 1 ? z.y : z.x) * a.scale2 : 0.f;
     }
-    floatx4_t o[8];
+    floatx4_t o[8];                                  // element 16 x + 4 gk + i
     float m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int x = 0; x < 8; ++x) o[x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
@@ -358,25 +388,41 @@ __global__ __launch_bounds__(256) void k_tree_rows_f32(const TreeArgs a)
         const bool counts = seen >> dt & 1u;
         const int page = counts ? table[(c0 + dt) >> a.block_bits] : 0, in_page = (c0 + dt) & ((1 << a.block_bits) - 1);
         const size_t rec = (((size_t)page * a.Hkv + g) << a.block_bits) + in_page;
-        auto decode = [&](const uint8_t *codes, const void *cb, int M, float *acc) {
+        // (all codes of the record are asked for at once, rows eight books at a time)
+        auto decode = [&](const uint8_t *codes, const void *cb, int M, float *acc) __attribute__((always_inline)) {
+            uint4_t w[2];
+            w[0] = *reinterpret_cast<const uint4_t *>(codes);
+            w[1] = M == 32 ? *reinterpret_cast<const uint4_t *>(codes + 16) : w[0];
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-            for (int c = 0; c < M; c += 4) {
-                const unsigned w = *reinterpret_cast<const unsigned *>(codes + c);
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const size_t at = (((size_t)g * M + c + u) * kK + (w >> (8 * u) & 255u)) * kD + de;
+            for (int c = 0; c < 32; c += 8) {
+                if (c >= M) break;
+                __builtin_amdgcn_sched_barrier(0);
+                uint4_t x[8][CB16 ? 1 : 2];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const unsigned code = w[c / 16][(c % 16 + u) / 4] >> (8 * (u & 3)) & 255u;
+                    const size_t at = (((size_t)g * M + c + u) * kK + code) * kD + de;
                     if constexpr (CB16) {
-                        const uint4_t x = *reinterpret_cast<const uint4_t *>(static_cast<const uint16_t *>(cb) + at);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) { acc[2 * e] += bf16_lo(x[e]); acc[2 * e + 1] += bf16_hi(x[e]); }
+                        x[u][0] = *reinterpret_cast<const uint4_t *>(static_cast<const uint16_t *>(cb) + at);
                     } else {
-                        const floatx4_t x = *reinterpret_cast<const floatx4_t *>(static_cast<const float *>(cb) + at);
-                        const floatx4_t y = *reinterpret_cast<const floatx4_t *>(static_cast<const float *>(cb) + at + 4);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) { acc[e] += x[e]; acc[4 + e] += y[e]; }
+                        x[u][0] = *reinterpret_cast<const uint4_t *>(static_cast<const float *>(cb) + at);
+                        x[u][1] = *reinterpret_cast<const uint4_t *>(static_cast<const float *>(cb) + at + 4);
                     }
                 }
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if constexpr (CB16) {
+                            const unsigned v = x[u][0][e / 2];
+                            acc[e] += e & 1 ? bf16_hi(v) : bf16_lo(v);
+                        } else {
+                            const unsigned v = x[u][e / 4][e & 3];
+                            acc[e] += __builtin_bit_cast(float, v);
+                        }
+                    }
             }
         };
         float x[8];
@@ -395,7 +441,7 @@ __global__ __launch_bounds__(256) void k_tree_rows_f32(const TreeArgs a)
         for (int e = 0; e < 8; ++e) ktile[dt * kWideRow + de + e] = x[e];
         decode(a.val_pages + rec * a.Mv, a.val_cb, a.Mv, x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) vtile[dt * kWideRow + de + e] = counts ? x[e] : 0.f;
+        for (int e = 0; e < 8; ++e) vtile[dt * kWideRow + de + e] = counts ? x[e] : 0.f;   // (a weight of zero does not hide an infinity)
         __syncthreads();
         floatx4_t sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -439,15 +485,14 @@ __global__ __launch_bounds__(256) void k_tree_rows_f32(const TreeArgs a)
 namespace {
 
 // ------------------------------------------------------------------ k_tree_final
-constexpr int kFinalWaves = 4;
-
-// A workgroup joins the parts of one row: a wavefront every fourth range and every fourth node that the row attends to, a lane one
-// sub-space.  The nodes' part is fp32 arithmetic, node by node: nodes outside the mask are not read, so that what they hold cannot matter.
-template <bool Q16>
-__global__ __launch_bounds__(64 * kFinalWaves) void k_tree_final(const TreeArgs a)
+// A workgroup joins the parts of one row: a wavefront a run of ranges and every W-th node that the row attends to, a lane one sub-space.
+// The nodes' part is fp32 arithmetic, node by node: nodes outside the mask are not read, so that what they hold cannot matter.
+// Bound by latency: the ranges' statistics are one load of the wavefront, their rows are asked for eight at a time, nodes two at a time.
+template <bool Q16, int W>
+__global__ __launch_bounds__(64 * W) void k_tree_final(const TreeArgs a)
 {
-    __shared__ float sm[kFinalWaves], sl[kFinalWaves];
-    __shared__ float2 so[kFinalWaves][kJ];
+    __shared__ float sm[W], sl[W];
+    __shared__ float2 so[W][kJ];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int node = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq, g = h / a.G;
     // the sequence: as many as end at or before this node come before it
@@ -459,45 +504,73 @@ __global__ __launch_bounds__(64 * kFinalWaves) void k_tree_final(const TreeArgs 
         if (ended < 64) break;
     }
     if (b >= a.batch) return;                         // a row behind the last sequence
+    const Span s = span_of(a, b);
+    const int i = node - s.n0;
+    const bool there = i >= 0 && i < s.n;
     float m = -INFINITY, l = 0.f;
     float2 o = make_float2(0.f, 0.f);
-    {
-        const Span s = span_of(a, b);
-        const int i = node - s.n0;
-        if (i >= 0 && i < s.n) {
-            const int ns = min((s.L + a.split_len - 1) / a.split_len * a.halves, a.splits);
-            const size_t row = (size_t)blockIdx.x * a.splits;
-            for (int k = wave; k < ns; k += kFinalWaves) {
-                const float2 st = a.stat[row + k];
-                const float2 v = *reinterpret_cast<const float2 *>(a.part + (row + k) * kD + 2 * lane);
-                if (st.x == -INFINITY) continue;      // (a range without a page)
-                const float now = fmaxf(m, st.x), x = __builtin_amdgcn_exp2f(m - now), y = __builtin_amdgcn_exp2f(st.x - now);
-                m = now;
-                l = l * x + st.y * y;
-                o.x = o.x * x + v.x * y;
-                o.y = o.y * x + v.y * y;
-            }
-            unsigned long long mask = a.mask ? a.mask[node] : ~0ull >> (63 - i);
-            if (s.n < 64) mask &= (1ull << s.n) - 1;
-            const int ax = axis_of(a, lane);
-            const size_t at = (size_t)node * a.q_stride + (size_t)h * kD + 2 * lane;
-            const float2 q = make_float2(cb_elem<Q16>(a.q, at) * a.scale2, cb_elem<Q16>(a.q, at + 1) * a.scale2);
-            const int own = a.turn ? a.node_pos[(size_t)node * a.n_axes + ax] : 0;
-            for (int k = 0; mask; mask &= mask - 1, ++k) {
-                if (k % kFinalWaves != wave) continue;
-                const int j = s.n0 + __builtin_ctzll(mask);
-                const size_t from = (size_t)j * a.node_stride + (size_t)g * kD + 2 * lane;
-                const float2 key = make_float2(cb_elem<Q16>(a.node_k, from), cb_elem<Q16>(a.node_k, from + 1));
-                const float2 val = make_float2(cb_elem<Q16>(a.node_v, from), cb_elem<Q16>(a.node_v, from + 1));
-                float2 z = q;
-                if (a.turn) z = times(q, turned_by(a, own - a.node_pos[(size_t)j * a.n_axes + ax], lane));
-                const float x = wave_sum(z.x * key.x + z.y * key.y);
-                const float now = fmaxf(m, x), base = now == -INFINITY ? 0.f : now;
-                const float was = __builtin_amdgcn_exp2f(m - base), w = __builtin_amdgcn_exp2f(x - base);
-                m = now;
-                l = l * was + w;
-                o.x = o.x * was + val.x * w;
-                o.y = o.y * was + val.y * w;
+
+    // nodes
+    unsigned long long mask = !there ? 0 : a.mask ? a.mask[node] : ~0ull >> (63 - i);
+    if (s.n < 64) mask &= (1ull << s.n) - 1;
+    const int ax = axis_of(a, lane);
+    const size_t at = (size_t)node * a.q_stride + (size_t)h * kD + 2 * lane;
+    const float2 q = make_float2(cb_elem<Q16>(a.q, at) * a.scale2, cb_elem<Q16>(a.q, at + 1) * a.scale2);
+    const int own = a.turn ? a.node_pos[(size_t)node * a.n_axes + ax] : 0;
+    for (int k = 0; k < wave; ++k) mask &= mask - 1;  // (a wavefront's first node)
+    while (mask) {
+        constexpr int U = 2;
+        float2 key[U], val[U], e[U];
+        bool is[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            is[u] = mask != 0;
+            const int j = s.n0 + (is[u] ? __builtin_ctzll(mask) : 0);
+            const size_t from = (size_t)j * a.node_stride + (size_t)g * kD + 2 * lane;
+            key[u] = make_float2(cb_elem<Q16>(a.node_k, from), cb_elem<Q16>(a.node_k, from + 1));
+            val[u] = make_float2(cb_elem<Q16>(a.node_v, from), cb_elem<Q16>(a.node_v, from + 1));
+            e[u] = a.turn ? turned_by(a, own - a.node_pos[(size_t)j * a.n_axes + ax], lane) : make_float2(1.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < W; ++k) mask &= mask - 1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!is[u]) break;
+            const float2 z = times(q, e[u]);
+            const float x = wave_sum(z.x * key[u].x + z.y * key[u].y);
+            const float now = fmaxf(m, x), base = now == -INFINITY ? 0.f : now;
+            const float was = __builtin_amdgcn_exp2f(m - base), w = __builtin_amdgcn_exp2f(x - base);
+            m = now;
+            l = l * was + w;
+            o.x = o.x * was + val[u].x * w;
+            o.y = o.y * was + val[u].y * w;
+        }
+    }
+
+    // ranges: those of a wavefront follow each other, 64 at a time
+    const int ns = there ? min((s.L + a.split_len - 1) / a.split_len * a.halves, a.splits) : 0, per = (ns + W - 1) / W;
+    const size_t row = (size_t)blockIdx.x * a.splits;
+    const int k_end = min(ns, (wave + 1) * per);
+    for (int k0 = wave * per; k0 < k_end; k0 += 64) {
+        const int here = min(64, k_end - k0);
+        const float2 st = lane < here ? a.stat[row + k0 + lane] : make_float2(-INFINITY, 0.f);
+        const float now = fmaxf(m, wave_max(st.x)), base = now == -INFINITY ? 0.f : now;
+        const float was = __builtin_amdgcn_exp2f(m - base), w = __builtin_amdgcn_exp2f(st.x - base);   // (a range without a page: 0)
+        m = now;
+        l = l * was + wave_sum(st.y * w);
+        o.x *= was;
+        o.y *= was;
+        const float *from = a.part + (row + k0) * kD + 2 * lane;
+        for (int k = 0; k < here; k += 8) {
+            float2 v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const float2 *>(from + (size_t)min(k + u, here - 1) * kD);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), min(k + u, here - 1)));
+                if (k + u >= here) break;
+                o.x += v[u].x * f;
+                o.y += v[u].y * f;
             }
         }
     }
@@ -508,9 +581,9 @@ __global__ __launch_bounds__(64 * kFinalWaves) void k_tree_final(const TreeArgs 
     float top = -INFINITY, sum = 0.f;
     float2 t = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int w = 0; w < kFinalWaves; ++w) top = fmaxf(top, sm[w]);
+    for (int w = 0; w < W; ++w) top = fmaxf(top, sm[w]);
 #pragma unroll
-    for (int w = 0; w < kFinalWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
         if (sl[w] == 0.f) continue;                   // (nothing there)
         const float f = __builtin_amdgcn_exp2f(sm[w] - top);
         sum += sl[w] * f;
@@ -540,7 +613,7 @@ __global__ __launch_bounds__(256) void k_tree_pack(const uint4 *__restrict__ cb,
 
 // ------------------------------------------------------------------ host side
 struct TreePlan {
-    int nr, rg;          // rows gathered: wavefronts and row tiles of a wavefront; decoded ahead: wavefronts of different rows
+    int nr, rg;          // rows gathered: wavefronts and row tiles of a wavefront; streamed: sets, 0; decoded ahead: wavefronts of different rows, sets
     int row_tiles, splits, split_len;
     int tiles_per_head;  // decoded ahead: row tiles of 16 of all sequences
     int pass_tiles, passes;  // decoded ahead: token tiles of a pass
@@ -558,8 +631,8 @@ void tree_room(const commvq_handle *h, int batch, int total_nodes, bool stream, 
     p.bytes = std::max<size_t>(256, stream ? p.q_at + (size_t)p.tiles_per_head * h->cfg.n_kv_heads * 4096 : p.q_at);
 }
 
-// Rows of a workgroup: the smallest of 16, 32, 64, 128 and 256 that holds the largest tree's.  Ranges: as many as fill the chip with 16 wavefronts a
-// compute unit, in whole chunks.
+// Rows of a workgroup: the smallest of 16, 32, 64, 128 and 256 that holds the largest tree's.  Ranges: in whole chunks, as many as give
+// every compute unit four workgroups.
 TreePlan rows_plan(const commvq_handle *h, int batch, int total_nodes, int max_nodes, int max_seqlen)
 {
     TreePlan p{};
@@ -571,7 +644,7 @@ TreePlan rows_plan(const commvq_handle *h, int batch, int total_nodes, int max_n
     const int chunk = wide(h->cfg) ? kWideChunk : kChunk;
     const int64_t units = (int64_t)batch * h->cfg.n_kv_heads * p.row_tiles;
     const int64_t chunks = (max_seqlen + chunk - 1) / chunk;
-    const int64_t want = std::max<int64_t>(1, 4096 / p.nr / units);
+    const int64_t want = std::max<int64_t>(1, 1024 / units);
     const int64_t per = std::max<int64_t>(1, (chunks + want - 1) / want);
     p.split_len = (int)per * chunk;
     p.splits = (int)((chunks + per - 1) / per);
@@ -579,20 +652,29 @@ TreePlan rows_plan(const commvq_handle *h, int batch, int total_nodes, int max_n
     return p;
 }
 
-// Ranges of k_tree_stream: whole tiles, so many a workgroup that the last round of workgroups (one per compute unit) ends soonest.
+// Tiles and ranges of k_tree_stream: of the tile sizes the one, and of whole tiles so many a workgroup, that the last round of workgroups (one
+// per compute unit) ends soonest.  A stage of 512, 1024 and 2048 tokens takes 0.9, 1.2 and 2.0 us (the first two wait for the transfer of the
+// next one): 16 codebooks each, 8 heads, whole calls with tiles of 512 | 1024 | 2048: 16 000 tokens 42.5 | 45.8 | 70.0 us, 32 768 77.9 | 51.4 | 73.2,
+// 65 536 146 | 99.1 | 83.5.
 TreePlan stream_plan(const commvq_handle *h, int batch, int total_nodes, int max_seqlen)
 {
     TreePlan p{};
     p.row_tiles = 1;
-    const int64_t units = (int64_t)batch * h->cfg.n_kv_heads, tiles = (max_seqlen + kStreamTile - 1) / kStreamTile;
+    const int64_t units = (int64_t)batch * h->cfg.n_kv_heads;
     double best = 0;
-    int64_t per = 1;
-    for (int64_t x = 1; x <= tiles; ++x) {
-        const double cost = (double)((units * ((tiles + x - 1) / x) + 255) / 256) * (x + 0.1);   // (a tenth of a tile for a workgroup's beginning)
-        if (x == 1 || cost < best) { best = cost; per = x; }
+    for (int sets = kStreamMaxSets; sets >= 2; sets /= 2) {
+        const int64_t tiles = (max_seqlen + stream_tile(sets) - 1) / stream_tile(sets);
+        const double tile_us = (h->cfg.m_key + h->cfg.m_val) * (sets == 8 ? 2.0 : sets == 4 ? 1.2 : 0.9);
+        for (int64_t x = 1; x <= tiles; ++x) {
+            const double cost = (double)((units * ((tiles + x - 1) / x) + 255) / 256) * (x * tile_us + 3.0);
+            if (p.nr == 0 || cost < best) {
+                best = cost;
+                p.nr = sets;
+                p.split_len = (int)x * stream_tile(sets);
+                p.splits = (int)((tiles + x - 1) / x);
+            }
+        }
     }
-    p.split_len = (int)per * kStreamTile;
-    p.splits = (int)((tiles + per - 1) / per);
     tree_room(h, batch, total_nodes, false, p);
     return p;
 }
@@ -606,29 +688,37 @@ TreePlan dense_plan(const commvq_handle *h, int batch, int total_nodes, int max_
     const int rows = max_nodes * h->G, groups = (rows + 16 * kDenseRows - 1) / (16 * kDenseRows), Hkv = h->cfg.n_kv_heads;
     p.nr = groups <= 1 ? 1 : groups <= 2 ? 2 : groups <= 4 ? 4 : 8;
     p.row_tiles = (groups + p.nr - 1) / p.nr;
-    const int tiles = (max_seqlen + kDecodeTile - 1) / kDecodeTile;
+    // tiles of 1024 tokens instead of 2048 where that saves rounds of workgroups: 0.62 of a large one's time (8 heads, 8 nodes, 16 codebooks, 1024 | 2048:
+    // 8000 tokens 53.8 | 59.3 us, 32 768 104.9 | 85.4; 32 sequences of 600 118.6 | 173.0, of 1500 204.6 | 174.3)
+    auto rounds = [&](int sets) { return ((int64_t)batch * ((max_seqlen + sets * kDecodeSetTokens - 1) / (sets * kDecodeSetTokens)) * Hkv * 2 + 255) / 256; };
+    p.rg = 0.62 * (double)rounds(2) < (double)rounds(4) ? 2 : 4;
+    const int tile = p.rg * kDecodeSetTokens, halves = p.rg * kDecodeWaves / kDenseSteps, tiles = (max_seqlen + tile - 1) / tile;
     const int64_t all = (int64_t)batch * tiles;
-    p.pass_tiles = (int)std::min<int64_t>(all, std::max(1, kDenseTileHeads / Hkv));
+    p.pass_tiles = (int)std::min<int64_t>(all, std::max(1, kDenseTileHeads * kDecodeMaxSets / p.rg / Hkv));
     p.passes = (int)((all + p.pass_tiles - 1) / p.pass_tiles);
-    p.split_len = kDecodeTile;
-    p.splits = std::min(tiles, p.pass_tiles) * kDenseHalves;
+    p.split_len = tile;
+    p.splits = std::min(tiles, p.pass_tiles) * halves;
     tree_room(h, batch, total_nodes, true, p);
-    const size_t steps = (size_t)p.pass_tiles * Hkv * kDecodeSteps;
+    const size_t steps = (size_t)p.pass_tiles * Hkv * p.rg * kDecodeWaves;
     p.keys_at = align_up(p.bytes, 256);
     p.vals_at = p.keys_at + steps * kStepBytes;
     p.seen_at = p.vals_at + steps * kStepBytes;
     p.phases_at = align_up(p.seen_at + steps * 4, 256);
-    p.bytes = p.phases_at + (size_t)p.pass_tiles * kDecodeSteps * 16 * 64 * 16;
+    p.bytes = p.phases_at + (size_t)p.pass_tiles * p.rg * kDecodeWaves * 16 * 64 * 16;
     return p;
 }
 
-// Which kernels a call takes.  (What the workspace is sized for does not depend on tables and positions, which are not known then.)
+// Which kernels a call takes.  (What the workspace is sized for does not depend on tables and positions, which are not known then.)  With u tokens
+// times KV heads, M the mean number of codebooks, 8 heads, rows gathered | the other way: up to 16 rows, M = 16: u = 16 000 28.6 | 36.4 us, 32 000
+// 48.5 | 37.1; M = 32: 32 000 62.7 | 73.1, 64 000 90.6 | 74.5.  32 rows, M = 16: 16 000 32.2 | 49.0, 32 000 54.7 | 50.9; 256 rows 66.5 | 86.4, 120 | 90.1;
+// M = 32: 72.2 | 104, 134 | 106.
 enum Way { kRows, kStream, kDense };
 Way tree_way(const commvq_handle *h, int batch, int max_nodes, int max_seqlen, bool tables, bool implicit)
 {
     if (wide(h->cfg) || !tables || max_seqlen < 1) return kRows;
-    if ((int64_t)batch * h->cfg.n_kv_heads * ((max_seqlen + 1023) / 1024) < 96) return kRows;
-    return max_nodes * h->G <= kStreamRows && implicit ? kStream : kDense;
+    const int64_t units = (int64_t)batch * h->cfg.n_kv_heads * max_seqlen;
+    if (max_nodes * h->G <= kStreamRows && implicit) return units < 650 * (h->cfg.m_key + h->cfg.m_val) ? kRows : kStream;
+    return units < 26000 ? kRows : kDense;
 }
 
 TreePlan plan_of(Way way, const commvq_handle *h, int batch, int total_nodes, int max_nodes, int max_seqlen)
@@ -649,51 +739,59 @@ commvq_status check_tree_sizes(const commvq_handle *h, int32_t batch, int32_t to
 template <int NR, int RG>
 hipError_t launch_rows(const TreeArgs &a, dim3 grid, hipStream_t s)
 {
-    if (a.n_axes > 1) k_tree_rows<NR, RG, true><<<grid, 64 * NR, 0, s>>>(a);
-    else k_tree_rows<NR, RG, false><<<grid, 64 * NR, 0, s>>>(a);
+    if (a.n_axes > 1) k_tree_rows<NR, RG, true><<<grid, 64 * kRowsWaves, 0, s>>>(a);
+    else k_tree_rows<NR, RG, false><<<grid, 64 * kRowsWaves, 0, s>>>(a);
     return hipGetLastError();
 }
 
 hipError_t launch_wide(const TreeArgs &a, dim3 grid, hipStream_t s)
 {
-    if (a.q_bf16) k_tree_rows_f32<true, false><<<grid, 256, 0, s>>>(a);
-    else if (a.cb_bf16) k_tree_rows_f32<false, true><<<grid, 256, 0, s>>>(a);
-    else k_tree_rows_f32<false, false><<<grid, 256, 0, s>>>(a);
+    if (a.q_bf16) k_tree_rows_f32<true, false><<<grid, kWideThreads, 0, s>>>(a);
+    else if (a.cb_bf16) k_tree_rows_f32<false, true><<<grid, kWideThreads, 0, s>>>(a);
+    else k_tree_rows_f32<false, false><<<grid, kWideThreads, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <int NBK, int NBV, int SETS>
+hipError_t launch_stream_as(const TreeArgs &a, const char *tables, dim3 grid, hipStream_t s)
+{
+    static std::atomic<uint64_t> lds_ok{0};
+    const hipError_t e = allow_dynamic_lds(k_tree_stream<NBK, NBV, SETS>, kTreeLds, lds_ok);
+    if (e != hipSuccess) return e;
+    k_tree_stream<NBK, NBV, SETS><<<grid, kStreamThreads, kTreeLds, s>>>(a, tables);
     return hipGetLastError();
 }
 
 template <int NBK, int NBV>
-hipError_t launch_stream_as(const TreeArgs &a, const char *tables, dim3 grid, hipStream_t s)
+hipError_t launch_stream_sets(const TreeArgs &a, int sets, const char *tables, dim3 grid, hipStream_t s)
 {
-    static std::atomic<uint64_t> lds_ok{0};
-    const hipError_t e = allow_dynamic_lds(k_tree_stream<NBK, NBV>, kTreeLds, lds_ok);
-    if (e != hipSuccess) return e;
-    k_tree_stream<NBK, NBV><<<grid, kStreamThreads, kTreeLds, s>>>(a, tables);
-    return hipGetLastError();
+    return sets == 8 ? launch_stream_as<NBK, NBV, 8>(a, tables, grid, s) : sets == 4 ? launch_stream_as<NBK, NBV, 4>(a, tables, grid, s)
+                                                                          : launch_stream_as<NBK, NBV, 2>(a, tables, grid, s);
 }
 
-hipError_t launch_stream(const TreeArgs &a, const char *tables, dim3 grid, hipStream_t s)
+hipError_t launch_stream(const TreeArgs &a, int sets, const char *tables, dim3 grid, hipStream_t s)
 {
-    if (a.Mk == 16) return a.Mv == 16 ? launch_stream_as<1, 1>(a, tables, grid, s) : launch_stream_as<1, 2>(a, tables, grid, s);
-    return a.Mv == 16 ? launch_stream_as<2, 1>(a, tables, grid, s) : launch_stream_as<2, 2>(a, tables, grid, s);
+    if (a.Mk == 16) return a.Mv == 16 ? launch_stream_sets<1, 1>(a, sets, tables, grid, s) : launch_stream_sets<1, 2>(a, sets, tables, grid, s);
+    return a.Mv == 16 ? launch_stream_sets<2, 1>(a, sets, tables, grid, s) : launch_stream_sets<2, 2>(a, sets, tables, grid, s);
 }
 
 bool explicit_positions(const TreeArgs &a) { return a.turn && (a.key_pos || a.n_axes > 1); }
 
+template <int NBK, int NBV, int SETS, bool EXPLICIT>
+hipError_t launch_decode_as(const TreeArgs &a, const DensePass &d, const char *tables, dim3 grid, hipStream_t s)
+{
+    static std::atomic<uint64_t> lds_ok{0};
+    const hipError_t e = allow_dynamic_lds(k_tree_decode<NBK, NBV, SETS, EXPLICIT>, kDecodeLds, lds_ok);
+    if (e != hipSuccess) return e;
+    k_tree_decode<NBK, NBV, SETS, EXPLICIT><<<grid, kDecodeThreads, kDecodeLds, s>>>(a, d, tables);
+    return hipGetLastError();
+}
+
 template <int NBK, int NBV>
 hipError_t launch_decode(const TreeArgs &a, const DensePass &d, const char *tables, dim3 grid, hipStream_t s)
 {
-    static std::atomic<uint64_t> ok0{0}, ok1{0};
-    if (explicit_positions(a)) {
-        const hipError_t e = allow_dynamic_lds(k_tree_decode<NBK, NBV, true>, kDecodeLds, ok1);
-        if (e != hipSuccess) return e;
-        k_tree_decode<NBK, NBV, true><<<grid, kDecodeThreads, kDecodeLds, s>>>(a, d, tables);
-    } else {
-        const hipError_t e = allow_dynamic_lds(k_tree_decode<NBK, NBV, false>, kDecodeLds, ok0);
-        if (e != hipSuccess) return e;
-        k_tree_decode<NBK, NBV, false><<<grid, kDecodeThreads, kDecodeLds, s>>>(a, d, tables);
-    }
-    return hipGetLastError();
+    if (explicit_positions(a)) return d.sets == 4 ? launch_decode_as<NBK, NBV, 4, true>(a, d, tables, grid, s) : launch_decode_as<NBK, NBV, 2, true>(a, d, tables, grid, s);
+    return d.sets == 4 ? launch_decode_as<NBK, NBV, 4, false>(a, d, tables, grid, s) : launch_decode_as<NBK, NBV, 2, false>(a, d, tables, grid, s);
 }
 
 template <int WR>
@@ -710,16 +808,16 @@ hipError_t launch_dense(const TreeArgs &a, const TreePlan &p, int passes, const 
 {
     DensePass d{workspace + p.keys_at, workspace + p.vals_at, reinterpret_cast<unsigned *>(workspace + p.seen_at),
                 reinterpret_cast<floatx4_t *>(workspace + p.phases_at), reinterpret_cast<uint4_t *>(workspace + p.q_at),
-                p.tiles_per_head, 0, p.pass_tiles, 0, (a.max_nodes * a.G + 15) / 16};
+                p.tiles_per_head, 0, p.pass_tiles, p.rg, p.rg * kDecodeSetTokens, p.rg * kDecodeWaves, 0, (a.max_nodes * a.G + 15) / 16};
     const int64_t turns = ((int64_t)a.batch * a.Hkv * d.turn_tiles + kDecodeWaves - 1) / kDecodeWaves;
-    const int64_t decode = 2ll * d.tiles * a.Hkv, dense = (int64_t)d.tiles * a.Hkv * p.row_tiles * kDenseHalves;
+    const int64_t decode = 2ll * d.tiles * a.Hkv, dense = (int64_t)d.tiles * a.Hkv * p.row_tiles * (d.steps / kDenseSteps);
     if (std::max(turns + decode, dense) > 0x7fffffff) return hipErrorInvalidValue;
     for (int i = 0; i < passes; ++i, d.tile0 += d.tiles) {
         d.turn_wgs = i == 0 ? (int)turns : 0;
         const dim3 first((unsigned)(d.turn_wgs + decode)), second((unsigned)dense);
         hipError_t e;
         if (explicit_positions(a)) {
-            k_tree_phases<<<dim3((unsigned)d.tiles * kDecodeSteps), 256, 0, s>>>(a, d);
+            k_tree_phases<<<dim3((unsigned)(d.tiles * d.steps)), 256, 0, s>>>(a, d);
             e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
@@ -791,7 +889,7 @@ commvq_status commvq_tree_attn(commvq_handle *h, const commvq_pages *pages, cons
     const Way way = tree_way(h, t->batch, t->max_nodes, t->max_seqlen, tables != nullptr, pages->n_axes == 1 && !t->key_pos);
     const TreePlan p = plan_of(way, h, t->batch, t->total_nodes, t->max_nodes, t->max_seqlen);
     // (what the device may hold of it beyond this is left out: whole tiles, sequence by sequence)
-    const int64_t tiles = t->total_tokens ? std::min<int64_t>((int64_t)p.pass_tiles * p.passes, t->total_tokens / kDecodeTile + t->batch) : (int64_t)p.pass_tiles * p.passes;
+    const int64_t tiles = t->total_tokens ? std::min<int64_t>((int64_t)p.pass_tiles * p.passes, t->total_tokens / std::max(1, p.split_len) + t->batch) : (int64_t)p.pass_tiles * p.passes;
     const int64_t wgs = (int64_t)t->batch * c.n_kv_heads * p.row_tiles * p.splits;
     if (wgs > 0x7fffffff) return COMMVQ_ERR_SHAPE;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < need) return COMMVQ_ERR_WORKSPACE;
@@ -809,7 +907,7 @@ commvq_status commvq_tree_attn(commvq_handle *h, const commvq_pages *pages, cons
     a.batch = t->batch; a.Hq = c.n_q_heads; a.Hkv = c.n_kv_heads; a.G = h->G; a.Mk = c.m_key; a.Mv = c.m_val; a.n_hi = h->n_hi;
     a.n_axes = pages->n_axes; a.block_bits = __builtin_ctz((unsigned)pages->block_size); a.n_blocks = pages->n_blocks; a.max_blocks = pages->max_blocks;
     a.total_nodes = t->total_nodes; a.max_nodes = t->max_nodes; a.max_seqlen = t->max_seqlen;
-    a.splits = p.splits; a.split_len = p.split_len; a.row_tiles = p.row_tiles; a.halves = way == kDense ? kDenseHalves : 1;
+    a.splits = p.splits; a.split_len = p.split_len; a.row_tiles = p.row_tiles; a.halves = way == kDense ? p.rg * kDecodeWaves / kDenseSteps : 1;
     a.turn = !c.position_free; a.q_bf16 = c.q_dtype == COMMVQ_BF16; a.cb_bf16 = c.codebook_dtype == COMMVQ_BF16;
     a.scale2 = h->scale * kLog2e;
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -817,7 +915,7 @@ commvq_status commvq_tree_attn(commvq_handle *h, const commvq_pages *pages, cons
         const dim3 grid((unsigned)wgs);
         hipError_t e;
         if (way == kDense) e = launch_dense(a, p, (int)((tiles + p.pass_tiles - 1) / p.pass_tiles), static_cast<const char *>(tables), static_cast<char *>(workspace), s);
-        else if (way == kStream) e = launch_stream(a, static_cast<const char *>(tables), grid, s);
+        else if (way == kStream) e = launch_stream(a, p.nr, static_cast<const char *>(tables), grid, s);
         else if (wide(c)) e = launch_wide(a, grid, s);
         else if (p.nr == 1) e = launch_rows<1, 1>(a, grid, s);
         else if (p.nr == 2) e = launch_rows<2, 1>(a, grid, s);
@@ -827,8 +925,15 @@ commvq_status commvq_tree_attn(commvq_handle *h, const commvq_pages *pages, cons
         if (e != hipSuccess) return COMMVQ_ERR_LAUNCH;
     }
     const dim3 rows((unsigned)((int64_t)t->total_nodes * c.n_q_heads));
-    if (a.q_bf16) k_tree_final<true><<<rows, 64 * kFinalWaves, 0, s>>>(a);
-    else k_tree_final<false><<<rows, 64 * kFinalWaves, 0, s>>>(a);
+    // sixteen wavefronts a row where there are many ranges or few rows
+    const bool many = p.splits > 32 && (int64_t)t->total_nodes * c.n_q_heads <= 1024;
+    if (many) {
+        if (a.q_bf16) k_tree_final<true, 16><<<rows, 64 * 16, 0, s>>>(a);
+        else k_tree_final<false, 16><<<rows, 64 * 16, 0, s>>>(a);
+    } else {
+        if (a.q_bf16) k_tree_final<true, 4><<<rows, 64 * 4, 0, s>>>(a);
+        else k_tree_final<false, 4><<<rows, 64 * 4, 0, s>>>(a);
+    }
     return hipGetLastError() == hipSuccess ? COMMVQ_OK : COMMVQ_ERR_LAUNCH;
 }
 

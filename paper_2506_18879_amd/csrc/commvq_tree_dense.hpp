@@ -5,15 +5,13 @@ namespace {
 
 constexpr int kDecodeWaves = 16;
 constexpr int kDecodeThreads = 64 * kDecodeWaves;
-constexpr int kDecodeSets = 4;                                       // sets of 32 tokens of a wavefront
-constexpr int kDecodeTile = 32 * kDecodeSets * kDecodeWaves;         // 2048 tokens = 64 fine positions x 32 coarse rows
-constexpr int kDecodeSteps = kDecodeSets * kDecodeWaves;             // sets of a tile
-constexpr int kDecodeCoarse = kDecodeTile / kLo;
+constexpr int kDecodeSetTokens = 32 * kDecodeWaves;                  // tokens of a tile for each set of 32 of a wavefront: 64 fine positions x 8 coarse rows
+constexpr int kDecodeMaxSets = 4;                                    // tiles of 2048 tokens, or of 1024 (two sets)
 constexpr int kStageBytes = 64 * 1024;                               // 16 codebooks x 256 codewords x 8 elements
 constexpr int kStepBytes = 32 * kD * 2;                              // 32 decoded keys (values)
 // LDS behind the two stages: coarse phase factors of the tile (keys), or a set's values on their way to columns, 1 KiB a wavefront
 constexpr int kAuxAt = 2 * kStageBytes;
-constexpr int kDecodeLds = kAuxAt + (kDecodeCoarse + 1) * kJ * 8;
+constexpr int kDecodeLds = kAuxAt + (8 * kDecodeMaxSets + 1) * kJ * 8;
 static_assert(kDecodeWaves * 1024 <= kDecodeLds - kAuxAt, "values' exchange fits");
 
 // What one pass of the two kernels has: tiles tile0 .. tile0 + tiles - 1 of the batch's (sequence by sequence), decoded into
@@ -25,6 +23,7 @@ struct DensePass {
     uint4_t *queries;    // [head][row tile of 16][k-step][lane], see turn_rows
     int tiles_per_head;  // row tiles of a head, of all sequences
     int tile0, tiles;
+    int sets, tile_tokens, steps;  // of a tile: sets of a wavefront, tokens, sets
     int turn_wgs, turn_tiles;  // workgroups of k_tree_decode that turn queries instead (first pass), row tiles of the largest tree
 };
 
@@ -32,12 +31,12 @@ struct DensePass {
 __host__ __device__ __forceinline__ int first_tile(int n0, int G, int b) { return n0 * G / 16 + b; }
 
 // The sequence and the place in it of tile t of the batch, by one wavefront; false if there are not so many.
-__device__ __forceinline__ bool find_tile(const TreeArgs &a, int t, int lane, int &b, int &at)
+__device__ __forceinline__ bool find_tile(const TreeArgs &a, int tile_tokens, int t, int lane, int &b, int &at)
 {
     int before = 0;
     for (int c = 0; c < a.batch; c += 64) {
         const int L = c + lane < a.batch ? min(max(a.seq_lens[c + lane], 0), a.max_seqlen) : 0;
-        const int own = (L + kDecodeTile - 1) / kDecodeTile;
+        const int own = (L + tile_tokens - 1) / tile_tokens;
         int incl = own;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
@@ -65,10 +64,10 @@ __device__ __forceinline__ void order() { asm volatile("" ::: "memory"); }
 // element that lane 16 gk + n has in place e (of 4) of the operands of a pair of slices
 __device__ __forceinline__ int slice_dim(int pair, int gk, int e) { return 16 * pair + 8 * (gk >> 1) + 4 * (gk & 1) + e; }
 
-// Decodes the keys (turned) or values of a tile of 2048 tokens of one head into the operands of k_tree_dense.
+// Decodes the keys (turned) or values of a tile of 2048 (1024) tokens of one head into the operands of k_tree_dense.
 // All codebooks of the head pass through LDS once per tile, 8 elements of 16 codebooks (64 KiB, a stage) at a time, in two buffers.
 //
-// Tokens.  A tile is 64 fine positions x 32 coarse rows of 64; wavefront w has fine positions 4 w .. + 3 of all rows, in four sets of 32 tokens:
+// Tokens.  A tile is 64 fine positions x 32 (16) coarse rows of 64; wavefront w has fine positions 4 w .. + 3 of all rows, in four (two) sets of 32 tokens:
 // token n of a set's first (second) half is fine position n % 4, coarse row 8 set + n / 4 (+ 4).  A lane's tokens then are whole coarse rows apart
 // and share the fine phase factor.  Per stage and set: the codes (registers for the whole tile) name 16-byte pieces in LDS, the matrix
 // cores add them (selection operand and order of the codebooks as in k_score_stream: no bank conflicts, whatever the codes), a lane gets four
@@ -76,11 +75,11 @@ __device__ __forceinline__ int slice_dim(int pair, int gk, int e) { return 16 * 
 // each half's token n.  Values: two slices of a set go through 1 KiB of LDS, written by token and read by columns (ds_read_b64_tr_b16).
 // Rounded to bf16, as a bf16 cache would hold them.
 // EXPLICIT: positions from the pool, or of several axes; the phase factors are k_tree_phases' then.
-template <int NB, bool KEYS, bool EXPLICIT>
+template <int NB, int kSets, bool KEYS, bool EXPLICIT>
 __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &d, const char *src, int g, int tile)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    constexpr int kSets = kDecodeSets;
+    constexpr int kTile = kSets * kDecodeSetTokens, kSteps = kSets * kDecodeWaves;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     auto send = [&](const char *from, int buf, int j) {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
@@ -88,12 +87,12 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
     };
     constexpr int SENDS = kStageBytes / (kDecodeThreads * 16);       // 4 per thread and stage
     int b = 0, at = 0;
-    if (!find_tile(a, d.tile0 + tile, lane, b, at)) return;          // (the same for the whole workgroup)
+    if (!find_tile(a, d.tile_tokens, d.tile0 + tile, lane, b, at)) return;          // (the same for the whole workgroup)
 #pragma unroll
     for (int j = 0; j < SENDS; ++j) send(src, 0, j);
     const Span s = span_of(a, b);
     const int n = lane & 15, gk = lane >> 4, par = gk & 1, second = gk >> 1;
-    const int c0 = at * kDecodeTile;
+    const int c0 = at * kTile;
 
     uint4_t sel;
     unsigned sidx;
@@ -140,7 +139,7 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
             }
         }
     }
-    const size_t step0 = ((size_t)tile * a.Hkv + g) * kDecodeSteps + wave * kSets;
+    const size_t step0 = ((size_t)tile * a.Hkv + g) * kSteps + wave * kSets;
     if (KEYS && lane == 0) {
 #pragma unroll
         for (int ts = 0; ts < kSets; ++ts) d.seen[step0 + ts] = (unsigned)(seen[ts] & 0xffffu) | (unsigned)(seen[ts] >> 32 & 0xffffu) << 16;
@@ -154,7 +153,7 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
     const int lo = lane_dist & (kLo - 1);
     const unsigned hi_at = kAuxAt + (unsigned)((lane_dist >> kLoBits) - H0) * (kJ * 8) + par * 16;
     if (KEYS && !EXPLICIT) {
-        for (int x = tid; x < (kDecodeCoarse + 1) * kJ; x += kDecodeThreads) {
+        for (int x = tid; x < (8 * kSets + 1) * kJ; x += kDecodeThreads) {
             const int H = H0 + x / kJ;
             float2 e = a.turn ? a.tbl_hi[(size_t)min((unsigned)(H < 0 ? -H : H), (unsigned)(a.n_hi - 1)) * kJ + (x & (kJ - 1))] : make_float2(1.f, 0.f);
             if (H < 0) e.y = -e.y;
@@ -163,7 +162,7 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
     }
 
     char *out = (KEYS ? d.keys : d.vals) + step0 * kStepBytes;
-    const floatx4_t *phases = d.phases + ((size_t)tile * kDecodeSteps + wave * kSets) * 16 * 64 + lane;
+    const floatx4_t *phases = d.phases + ((size_t)tile * kSteps + wave * kSets) * 16 * 64 + lane;
     const unsigned wave_at = kAuxAt + (unsigned)wave * 1024u;
     constexpr int kAhead = 3;
     auto fine = [&](int sl) { return *reinterpret_cast<const floatx4_t *>(a.tbl_lo + (size_t)lo * kJ + 4 * sl + 2 * par); };
@@ -322,12 +321,12 @@ __device__ __forceinline__ void turn_rows(const TreeArgs &a, const DensePass &d,
 // Phase factors of the tokens of a pass's tiles, for all heads; a thread has the two sub-spaces that the lane of k_tree_decode turns.
 __global__ __launch_bounds__(256) void k_tree_phases(const TreeArgs a, const DensePass d)
 {
-    const int step = blockIdx.x % kDecodeSteps, tile = blockIdx.x / kDecodeSteps, lane = threadIdx.x & 63;
+    const int step = blockIdx.x % d.steps, tile = blockIdx.x / d.steps, lane = threadIdx.x & 63;
     int b = 0, at = 0;
-    if (!find_tile(a, d.tile0 + tile, lane, b, at)) return;
+    if (!find_tile(a, d.tile_tokens, d.tile0 + tile, lane, b, at)) return;
     const Span s = span_of(a, b);
     const int n = lane & 15, par = lane >> 4 & 1, second = lane >> 5;
-    const int tok = at * kDecodeTile + 4 * (step / kDecodeSets) + (n & 3) + kLo * (n >> 2) + kLo * (8 * (step % kDecodeSets) + 4 * second);
+    const int tok = at * d.tile_tokens + 4 * (step / d.sets) + (n & 3) + kLo * (n >> 2) + kLo * (8 * (step % d.sets) + 4 * second);
     const int page = tok < s.L ? a.tables[(size_t)b * a.max_blocks + (tok >> a.block_bits)] : -1;
     const bool there = page >= 0 && page < a.n_blocks;
     const int32_t *own = a.key_pos && there ? a.key_pos + (((size_t)page << a.block_bits) + (tok & ((1 << a.block_bits) - 1))) * a.n_axes : nullptr;
@@ -349,7 +348,7 @@ __global__ __launch_bounds__(256) void k_tree_phases(const TreeArgs a, const Den
 
 // Workgroups: some that turn queries (first pass), then keys and values of every (tile, head); neighbours in the grid have different heads, so
 // that with 8 of them an XCD's L2 serves one.
-template <int NBK, int NBV, bool EXPLICIT>
+template <int NBK, int NBV, int SETS, bool EXPLICIT>
 __global__ __launch_bounds__(kDecodeThreads) void k_tree_decode(const TreeArgs a, const DensePass d, const char *__restrict__ packed)
 {
     int id = blockIdx.x;
@@ -361,19 +360,19 @@ __global__ __launch_bounds__(kDecodeThreads) void k_tree_decode(const TreeArgs a
     const int g = id % a.Hkv;
     id /= a.Hkv;
     const int tile = id % d.tiles;
-    if (id < d.tiles) decode_tile<NBK, true, EXPLICIT>(a, d, packed + (size_t)g * 16 * NBK * kStageBytes, g, tile);
-    else decode_tile<NBV, false, false>(a, d, packed + (size_t)(a.Hkv * NBK + g * NBV) * 16 * kStageBytes, g, tile);
+    if (id < d.tiles) decode_tile<NBK, SETS, true, EXPLICIT>(a, d, packed + (size_t)g * 16 * NBK * kStageBytes, g, tile);
+    else decode_tile<NBV, SETS, false, false>(a, d, packed + (size_t)(a.Hkv * NBK + g * NBV) * 16 * kStageBytes, g, tile);
 }
 
 // ------------------------------------------------------------------ k_tree_dense
-// Attention over decoded tiles: a workgroup has half a tile of one head (32 steps of 32 tokens) and 32 WR rows, WR of its wavefronts different rows,
+// Attention over decoded tiles: a workgroup has 32 steps of 32 tokens of one head, half of a large tile, and 32 WR rows, WR of its wavefronts different rows,
 // 8 / WR of them different steps.  Operands need no exchange: logits = K Q^T with tokens as rows, whose weights are the operand of V^T P^T.
 // With up to 64 rows they come from memory as they are (keys of the next step travel during the second product, values during the first); with more, four
 // or eight wavefronts need the same step, which then goes from memory into one of three buffers in LDS, two rounds ahead.
 // Parts of a sequence's tiles that are a whole pass apart are added up where the first of them left its own.
 constexpr int kDenseWaves = 8;
 constexpr int kDenseRows = 2;                                        // row tiles of a wavefront
-constexpr int kDenseHalves = 2;                                      // workgroups of a tile
+constexpr int kDenseSteps = 32;
 constexpr int kDenseBuffers = 3;
 constexpr int kMeet = 36;                                            // floats of a lane's row tile on its way to another wavefront: 32 sums, maximum, sum
 constexpr bool dense_shared(int wr) { return wr >= 4; }
@@ -385,23 +384,23 @@ constexpr int dense_lds(int wr)
 template <int WR>
 __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs a, const DensePass d)
 {
-    constexpr int WT = kDenseWaves / WR, RT = kDenseRows, STEPS = kDecodeSteps / kDenseHalves;
+    constexpr int WT = kDenseWaves / WR, RT = kDenseRows, STEPS = kDenseSteps;
     constexpr bool SHARED = dense_shared(WR);
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, gk = lane >> 4;
     int id = blockIdx.x;
     const int g = id % a.Hkv;
     id /= a.Hkv;
-    const int half = id % kDenseHalves;
-    id /= kDenseHalves;
+    const int halves = d.steps / STEPS, half = id % halves;
+    id /= halves;
     const int tile = id % d.tiles, rt0 = id / d.tiles;
     int b = 0, at = 0;
-    if (!find_tile(a, d.tile0 + tile, lane, b, at)) return;
+    if (!find_tile(a, d.tile_tokens, d.tile0 + tile, lane, b, at)) return;
     const Span s = span_of(a, b);
     const int R = s.n * a.G, wr = wave % WR, wt = wave / WR, rows0 = rt0 * WR * 16 * RT, r0 = rows0 + wr * 16 * RT;
     if (rows0 >= R) return;
     const int tiles16 = (R + 15) / 16;
-    const size_t step0 = ((size_t)tile * a.Hkv + g) * kDecodeSteps + half * STEPS;
+    const size_t step0 = ((size_t)tile * a.Hkv + g) * d.steps + half * STEPS;
 
     // SHARED: round i's steps WT i .. + WT - 1 into buffer i % 3, in pieces of 1 KiB; behind the last round it once more, for nothing
     constexpr int PIECES = WT * 2 * kStepBytes / 1024 / kDenseWaves; // of a wavefront and round
@@ -571,7 +570,7 @@ __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs 
     for (int rt = 0; rt < RT; ++rt) {
         const int r = r0 + 16 * rt + n;
         if (r >= R) continue;
-        const size_t row = ((size_t)(s.n0 + r / a.G) * a.Hq + g * a.G + r % a.G) * a.splits + at % d.tiles * kDenseHalves + half;
+        const size_t row = ((size_t)(s.n0 + r / a.G) * a.Hq + g * a.G + r % a.G) * a.splits + at % d.tiles * halves + half;
         float *to = a.part + row * kD + 8 * (gk & 1) + 4 * (gk >> 1);  // (slot 4 gk + i of slices 2 x, 2 x + 1: see decode_tile's columns)
         if (at >= d.tiles) {
             const float2 st = a.stat[row];

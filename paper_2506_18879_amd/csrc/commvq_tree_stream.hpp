@@ -6,15 +6,15 @@ namespace {
 constexpr int kStreamWaves = 8;
 constexpr int kStreamThreads = 64 * kStreamWaves;
 constexpr int kStreamRows = 16;
-constexpr int kStreamSets = 8;                                       // sets of 32 tokens of a wavefront
-constexpr int kStreamTile = 32 * kStreamWaves * kStreamSets;         // 2048 tokens = 64 fine positions x 32 coarse rows
-constexpr int kStreamCoarse = kStreamTile / kLo;
+constexpr int kStreamMaxSets = 8;                                    // sets of 32 tokens of a wavefront: 8, 4 or 2
+constexpr int stream_tile(int sets) { return 32 * kStreamWaves * sets; }   // 64 fine positions x 4 coarse rows a set
+constexpr int kStreamMaxTile = stream_tile(kStreamMaxSets);
 // LDS behind the two stages.  Key stages: coarse phase factors of the tile [33 rows][64], row maxima [8 wavefronts][16], slots [set][wavefront][32];
 // value stages, over the phase factors: per wavefront 1 KiB for one set's values on their way to columns, then for its sums of 16 elements [lane][4].
 // All stages: the queries [pair of slices][lane][4 bf16].
-constexpr int kMaxAt = kAuxAt + (kStreamCoarse + 1) * kJ * 8;
+constexpr int kMaxAt = kAuxAt + (kStreamMaxTile / kLo + 1) * kJ * 8;
 constexpr int kSlotAt = kMaxAt + kStreamWaves * kStreamRows * 4;
-constexpr int kQueryAt = kSlotAt + kStreamTile * 4;
+constexpr int kQueryAt = kSlotAt + kStreamMaxTile * 4;
 constexpr int kTreeLds = kQueryAt + 8 * 64 * 8;
 static_assert(kTreeLds <= kLdsBytes && kStreamWaves * 1024 <= kMaxAt - kAuxAt, "fits a compute unit");
 
@@ -37,7 +37,7 @@ typedef __attribute__((address_space(3))) floatx4_t *tree_f4_out;
 // (ds_read_b64_tr_b16), into sums for 16 elements += V^T P^T; these meet in LDS across the wavefronts and are added to the rows' parts
 // in memory (the range's earlier tiles, scaled to the new maximum).
 // NBK, NBV: stages of a slice of keys and of values (codebooks / 16).
-template <int NBK, int NBV>
+template <int NBK, int NBV, int SETS>
 __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a, const char *__restrict__ packed)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                      : : "s"((unsigned)(buf * kStageBytes + j * (kStreamThreads * 16) + wave * 1024)), "v"((unsigned)tid * 16u), "s"(src + j * (kStreamThreads * 16)));
     };
-    constexpr int kSets = kStreamSets, kTile = kStreamTile, kCoarse = kStreamCoarse;
+    constexpr int kSets = SETS, kTile = stream_tile(SETS), kCoarse = kTile / kLo;
     constexpr int SENDS = kStageBytes / (kStreamThreads * 16);    // 8 per thread and stage
 #pragma unroll
     for (int j = 0; j < SENDS; ++j) send(ksrc, 0, j);
