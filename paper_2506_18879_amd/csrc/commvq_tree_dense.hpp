@@ -33,6 +33,11 @@ __host__ __device__ __forceinline__ int first_tile(int n0, int G, int b) { retur
 // The sequence and the place in it of tile t of the batch, by one wavefront; false if there are not so many.
 __device__ __forceinline__ bool find_tile(const TreeArgs &a, int tile_tokens, int t, int lane, int &b, int &at)
 {
+    if (a.batch == 1) {
+        b = 0;
+        at = t;
+        return (long long)t * tile_tokens < min(max(a.seq_lens[0], 0), a.max_seqlen);
+    }
     int before = 0;
     for (int c = 0; c < a.batch; c += 64) {
         const int L = c + lane < a.batch ? min(max(a.seq_lens[c + lane], 0), a.max_seqlen) : 0;
@@ -72,7 +77,7 @@ __device__ __forceinline__ int slice_dim(int pair, int gk, int e) { return 16 * 
 // and share the fine phase factor.  Per stage and set: the codes (registers for the whole tile) name 16-byte pieces in LDS, the matrix
 // cores add them (selection operand and order of the codebooks as in k_score_stream: no bank conflicts, whatever the codes), a lane gets four
 // elements of one token.  Keys: it turns its two sub-spaces; the wavefront's halves of two slices are exchanged, so that a lane has 4 elements of
-// each half's token n.  Values: two slices of a set go through 1 KiB of LDS, written by token and read by columns (ds_read_b64_tr_b16).
+// each half's token n, and leaves them four slices at a time.  Values: two slices of a set go through 1 KiB of LDS, written by token and read by columns (ds_read_b64_tr_b16).
 // Rounded to bf16, as a bf16 cache would hold them.
 // EXPLICIT: positions from the pool, or of several axes; the phase factors are k_tree_phases' then.
 template <int NB, int kSets, bool KEYS, bool EXPLICIT>
@@ -86,10 +91,13 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
                      : : "s"((unsigned)(buf * kStageBytes + j * (kDecodeThreads * 16) + wave * 1024)), "v"((unsigned)tid * 16u), "s"(from + j * (kDecodeThreads * 16)));
     };
     constexpr int SENDS = kStageBytes / (kDecodeThreads * 16);       // 4 per thread and stage
-    int b = 0, at = 0;
-    if (!find_tile(a, d.tile_tokens, d.tile0 + tile, lane, b, at)) return;          // (the same for the whole workgroup)
 #pragma unroll
     for (int j = 0; j < SENDS; ++j) send(src, 0, j);
+    int b = 0, at = 0;
+    if (!find_tile(a, d.tile_tokens, d.tile0 + tile, lane, b, at)) {                // (the same for the whole workgroup)
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        return;
+    }
     const Span s = span_of(a, b);
     const int n = lane & 15, gk = lane >> 4, par = gk & 1, second = gk >> 1;
     const int c0 = at * kTile;
@@ -170,17 +178,17 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
     floatx4_t e_next = {1.f, 0.f, 1.f, 0.f};
     if (FINE && a.turn) e_next = fine(0);
 #pragma unroll 1
-    for (int pr = 0; pr < 8; ++pr) {
-        uint2_t kw[kSets];
+    for (int ks = 0; ks < 4; ++ks) {
+        uint2_t kw[kSets], ka[kSets], kb[kSets];                     // (keys: of the first two slices, halves A and B)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int sl = 2 * pr + i;
+        for (int i = 0; i < 4; ++i) {
+            const int sl = 4 * ks + i;
             floatx4_t e_lo, e_hi, acc[kSets];
 #pragma unroll
             for (int blk = 0; blk < NB; ++blk) {
                 const int buf = (NB * i + blk) & 1;
                 // this stage's transfers have landed; the results of the last one, sent off after them, may still be on their way
-                if (blk == 0 && i == 0 && pr > 0) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(KEYS ? 2 * kSets : kSets) : "memory");
+                if (blk == 0 && ((i == 0 && ks > 0) || (i == 2 && !KEYS))) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(KEYS ? 2 * kSets : kSets) : "memory");
                 else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
                 __builtin_amdgcn_s_barrier();
                 order();
@@ -215,20 +223,25 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
                             w[2 * u + 1] = z[2 * u + 1] * ex - z[2 * u] * ey;
                         }
                         const uint2_t k = {pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])};
-                        if (i == 0) {
+                        if (i % 2 == 0) {
                             kw[ts] = k;
                             return;
                         }
-                        uint2_t ka, kb;                              // tokens of halves A and B
+                        uint2_t xa, xb;                              // tokens of halves A and B
 #pragma unroll
                         for (int r = 0; r < 2; ++r) {
                             auto x = __builtin_amdgcn_permlane32_swap(kw[ts][r], k[r], false, false);
-                            ka[r] = x[0];
-                            kb[r] = x[1];
+                            xa[r] = x[0];
+                            xb[r] = x[1];
                         }
-                        char *to = out + ts * kStepBytes + pr * 512 + lane * 8;
-                        *reinterpret_cast<uint2_t *>(to) = ka;
-                        *reinterpret_cast<uint2_t *>(to + 4096) = kb;
+                        if (i == 1) {
+                            ka[ts] = xa;
+                            kb[ts] = xb;
+                            return;
+                        }
+                        char *to = out + ts * kStepBytes + ks * 1024 + lane * 16;
+                        *reinterpret_cast<uint4_t *>(to) = uint4_t{ka[ts][0], ka[ts][1], xa[0], xa[1]};
+                        *reinterpret_cast<uint4_t *>(to + 4096) = uint4_t{kb[ts][0], kb[ts][1], xb[0], xb[1]};
                     } else {
                         if (slot != 1 && slot != 4) return;
                         const int ts = 2 * p + slot / 4;
@@ -236,7 +249,7 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
                         // (a weight of zero does not hide an infinity: tokens that do not count are cleared)
                         asm("v_cndmask_b32 %0, 0, %0, %1" : "+v"(v[0]) : "s"(seen[ts]));
                         asm("v_cndmask_b32 %0, 0, %0, %1" : "+v"(v[1]) : "s"(seen[ts]));
-                        if (i == 0) {
+                        if (i % 2 == 0) {
                             kw[ts] = v;
                             return;
                         }
@@ -247,7 +260,7 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
                         const uint2_t x0 = __builtin_bit_cast(uint2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_ptr)(from)));
                         const uint2_t x1 = __builtin_bit_cast(uint2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_ptr)(from + 512u)));
                         order();
-                        *reinterpret_cast<uint4_t *>(out + ts * kStepBytes + pr * 1024 + lane * 16) = uint4_t{x0[0], x0[1], x1[0], x1[1]};
+                        *reinterpret_cast<uint4_t *>(out + ts * kStepBytes + (2 * ks + i / 2) * 1024 + lane * 16) = uint4_t{x0[0], x0[1], x1[0], x1[1]};
                     }
                 };
                 // The gather sums: steps of one read for each half of a set, sets two by two so that no matrix instruction waits for the one before
@@ -364,6 +377,17 @@ __global__ __launch_bounds__(kDecodeThreads) void k_tree_decode(const TreeArgs a
     else decode_tile<NBV, SETS, false, false>(a, d, packed + (size_t)(a.Hkv * NBK + g * NBV) * 16 * kStageBytes, g, tile);
 }
 
+// The maximum over lanes l, l ^ 16, l ^ 32 and l ^ 48.
+__device__ __forceinline__ float quads_max(float v)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const unsigned a0 = a[0], a1 = a[1], w = __builtin_bit_cast(unsigned, fmaxf(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1)));
+    auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    const unsigned b0 = b[0], b1 = b[1];
+    return fmaxf(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
+}
+
 // ------------------------------------------------------------------ k_tree_dense
 // Attention over decoded tiles: a workgroup has 32 steps of 32 tokens of one head, half of a large tile, and 32 WR rows, WR of its wavefronts different rows,
 // 8 / WR of them different steps.  Operands need no exchange: logits = K Q^T with tokens as rows, whose weights are the operand of V^T P^T.
@@ -394,12 +418,7 @@ __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs 
     const int halves = d.steps / STEPS, half = id % halves;
     id /= halves;
     const int tile = id % d.tiles, rt0 = id / d.tiles;
-    int b = 0, at = 0;
-    if (!find_tile(a, d.tile_tokens, d.tile0 + tile, lane, b, at)) return;
-    const Span s = span_of(a, b);
-    const int R = s.n * a.G, wr = wave % WR, wt = wave / WR, rows0 = rt0 * WR * 16 * RT, r0 = rows0 + wr * 16 * RT;
-    if (rows0 >= R) return;
-    const int tiles16 = (R + 15) / 16;
+    const int wr = wave % WR, wt = wave / WR;
     const size_t step0 = ((size_t)tile * a.Hkv + g) * d.steps + half * STEPS;
 
     // SHARED: round i's steps WT i .. + WT - 1 into buffer i % 3, in pieces of 1 KiB; behind the last round it once more, for nothing
@@ -413,10 +432,19 @@ __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs 
             lds_dma16(from, (unsigned)lane * 16u, (unsigned)(i % kDenseBuffers * (WT * 2 * kStepBytes) + piece * 1024));
         }
     };
-    if constexpr (SHARED) {
+    if constexpr (SHARED) {                                          // (the scratch is there, whether the tile is or not)
         send_round(0);
         send_round(1);
     }
+    int b = 0, at = 0;
+    const bool found = find_tile(a, d.tile_tokens, d.tile0 + tile, lane, b, at);
+    const Span s = span_of(a, b);
+    const int R = s.n * a.G, rows0 = rt0 * WR * 16 * RT, r0 = rows0 + wr * 16 * RT;
+    if (!found || rows0 >= R) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        return;
+    }
+    const int tiles16 = (R + 15) / 16;
 
     uint4_t qv[RT][4];
 #pragma unroll
@@ -434,13 +462,13 @@ __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs 
 #pragma unroll
         for (int x = 0; x < 8; ++x) o[rt][x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
     }
-    const char *kp = d.keys + step0 * kStepBytes + lane * 8, *vp = d.vals + step0 * kStepBytes + lane * 16;
-    uint2_t kv[2][8];
+    const char *kp = d.keys + step0 * kStepBytes + lane * 16, *vp = d.vals + step0 * kStepBytes + lane * 16;
+    uint4_t kv[2][4];
     auto load_keys = [&](const char *from) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int p = 0; p < 8; ++p) kv[h][p] = *reinterpret_cast<const uint2_t *>(from + h * 4096 + p * 512);
+            for (int ks = 0; ks < 4; ++ks) kv[h][ks] = *reinterpret_cast<const uint4_t *>(from + h * 4096 + ks * 1024);
     };
     if constexpr (!SHARED) load_keys(kp + (size_t)wt * kStepBytes);
     unsigned seen = d.seen[step0 + wt];
@@ -456,7 +484,7 @@ __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs 
             asm volatile("" ::: "memory");
             send_round(round + 2);
             const char *step = lds + round % kDenseBuffers * (WT * 2 * kStepBytes) + wt * 2 * kStepBytes;
-            load_keys(step + lane * 8);
+            load_keys(step + lane * 16);
 #pragma unroll
             for (int x = 0; x < 8; ++x) vv[x] = *reinterpret_cast<const uint4_t *>(step + kStepBytes + x * 1024 + lane * 16);
         } else {
@@ -471,10 +499,9 @@ __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs 
         for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint4_t k = {kv[h][2 * ks][0], kv[h][2 * ks][1], kv[h][2 * ks + 1][0], kv[h][2 * ks + 1][1]};
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
-                    sc[rt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, k), __builtin_bit_cast(bf16x8_t, qv[rt][ks]), sc[rt][h], 0, 0, 0);
+                    sc[rt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kv[h][ks]), __builtin_bit_cast(bf16x8_t, qv[rt][ks]), sc[rt][h], 0, 0, 0);
             }
         const unsigned now_seen = seen;
         const int next = min(st + WT, STEPS - 1);                    // (behind the last step: once more, not used)
@@ -497,28 +524,32 @@ __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs 
         uint4_t pv[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
+            // weights are relative to a number that is raised to the maximum only when a logit is more than 2^8 above it: rarely after the first
+            // steps, and neither sums nor weights (bf16: relative) care for a factor of 256
             float top = -INFINITY;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[rt][h][i]);
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float now = fmaxf(m[rt], top), base = now == -INFINITY ? 0.f : now, old = __builtin_amdgcn_exp2f(m[rt] - base);
-            m[rt] = now;
+            if (__ballot(top > m[rt] + 8.f)) {
+                top = quads_max(top);
+                const float now = fmaxf(m[rt], top), old = __builtin_amdgcn_exp2f(m[rt] - now);   // (a lane without any: -inf - -inf, not used)
+                const float f = m[rt] == -INFINITY ? 0.f : old;
+                m[rt] = now;
+                l[rt] *= f;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) o[rt][x] *= f;
+            }
+            const float base = m[rt] == -INFINITY ? 0.f : m[rt];
             float w[8], sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 w[i] = __builtin_amdgcn_exp2f(sc[rt][i / 4][i & 3] - base);
                 sum += w[i];
             }
-            l[rt] = l[rt] * old + sum;
+            l[rt] += sum;
 #pragma unroll
             for (int i = 0; i < 4; ++i) pv[rt][i] = pack_bf16(w[2 * i], w[2 * i + 1]);
-            if (__ballot(old != 1.f)) {                              // (rare after the first steps)
-#pragma unroll
-                for (int x = 0; x < 8; ++x) o[rt][x] *= old;
-            }
         }
 #pragma unroll
         for (int x = 0; x < 8; ++x)
@@ -531,6 +562,23 @@ __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs 
     for (int rt = 0; rt < RT; ++rt) {
         l[rt] += __shfl_xor(l[rt], 16);
         l[rt] += __shfl_xor(l[rt], 32);
+    }
+    // where the rows' parts go; what a pass before has left there is asked for before the wavefronts meet
+    float *to[RT];
+    size_t part_row[RT];
+    floatx4_t was[RT][8];
+    float2 was_stat[RT];
+    const bool again = at >= d.tiles;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int r = min(r0 + 16 * rt + n, R - 1);
+        part_row[rt] = ((size_t)(s.n0 + r / a.G) * a.Hq + g * a.G + r % a.G) * a.splits + at % d.tiles * halves + half;
+        to[rt] = a.part + part_row[rt] * kD + 8 * (gk & 1) + 4 * (gk >> 1);   // (slot 4 gk + i of slices 2 x, 2 x + 1: see decode_tile's columns)
+        if (again && wt == 0) {
+            was_stat[rt] = a.stat[part_row[rt]];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) was[rt][x] = *reinterpret_cast<const floatx4_t *>(to[rt] + 16 * x);
+        }
     }
     auto add = [&](int rt, float mo, float lo, auto other) __attribute__((always_inline)) {
         const float now = fmaxf(m[rt], mo), base = now == -INFINITY ? 0.f : now;
@@ -570,15 +618,10 @@ __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs 
     for (int rt = 0; rt < RT; ++rt) {
         const int r = r0 + 16 * rt + n;
         if (r >= R) continue;
-        const size_t row = ((size_t)(s.n0 + r / a.G) * a.Hq + g * a.G + r % a.G) * a.splits + at % d.tiles * halves + half;
-        float *to = a.part + row * kD + 8 * (gk & 1) + 4 * (gk >> 1);  // (slot 4 gk + i of slices 2 x, 2 x + 1: see decode_tile's columns)
-        if (at >= d.tiles) {
-            const float2 st = a.stat[row];
-            add(rt, st.x, st.y, [&](int x) { return *reinterpret_cast<const floatx4_t *>(to + 16 * x); });
-        }
+        if (again) add(rt, was_stat[rt].x, was_stat[rt].y, [&](int x) { return was[rt][x]; });
 #pragma unroll
-        for (int x = 0; x < 8; ++x) *reinterpret_cast<floatx4_t *>(to + 16 * x) = o[rt][x];
-        if (gk == 0) a.stat[row] = make_float2(m[rt], l[rt]);
+        for (int x = 0; x < 8; ++x) *reinterpret_cast<floatx4_t *>(to[rt] + 16 * x) = o[rt][x];
+        if (gk == 0) a.stat[part_row[rt]] = make_float2(m[rt], l[rt]);
     }
 }
 
