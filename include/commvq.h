@@ -5,7 +5,8 @@
  * Every cached key and value is stored as M uint8 code indices into learned
  * codebooks (additive quantization, paper Sec. 4.1, Eq. vanilla_decode), or in
  * the paper's own record formats (commvq_key_format, commvq_value_format).  The
- * library never decompresses the cache.  Scores follow the commutative
+ * library never decompresses the cache (commvq_tree_attn apart, whose many rows
+ * share a tile's decoded keys and values).  Scores follow the commutative
  * reformulation of Sec. 4.2 (Eq. new_attention): the selected key codewords are
  * gather-summed, rotated once by the RoPE matrix of the relative position and
  * contracted with the query.  Values follow the re-association of
@@ -369,7 +370,8 @@ typedef struct {
     int32_t q_stride;            /* elements from one node's queries to the next one's; 0: Hq * d (packed) */
     int32_t node_stride;         /* the same for node_keys and node_vals; 0: Hkv * d */
     int64_t total_tokens;        /* host copy of the sum of seq_lens, or 0: not known.  Long ragged batches of many rows are taken in
-                                    fewer steps with it; sequences behind the first total_tokens (in whole tiles of 2048) are not attended to */
+                                    fewer steps with it; where seq_lens holds more than it says, the rows of the last
+                                    sequences are not defined */
 } commvq_tree;
 
 /*
@@ -410,8 +412,8 @@ commvq_status commvq_store_pages(commvq_handle *handle, const commvq_pages *page
  * tokens of its sequence and to the nodes j that its mask names, whose keys and values are given as they are:
  *     out[i][h] = Softmax over both of ( (q_i R_t_i) . (k R_p) * scale ) . v
  * with k, v the decoded cache as in commvq_decode_attn, or node_keys[j], node_vals[j] (keys before RoPE).  One node per sequence
- * is single-token decoding over pages.  A node that attends to nothing gets zeros, rows of out behind the last sequence's nodes are left as they were; keys and values of nodes that a node does not
- * attend to do not touch it, whatever they hold.
+ * is single-token decoding over pages.  A node that attends to nothing gets zeros; rows of out behind the last sequence's nodes are
+ * left as they were; keys and values of nodes that a node does not attend to do not touch it, whatever they hold.
  *   q                    [N][Hq][d], q_dtype;  node_keys, node_vals  [N][Hkv][d], q_dtype;  out  [N][Hq][d], q_dtype
  *   key_pages, val_pages as above;  key_codebooks, val_codebooks  as for commvq_decode_attn in index form
  *   tables               what commvq_tree_prepare made of the codebooks, or NULL: rows are then gathered from the codebooks,
@@ -419,8 +421,10 @@ commvq_status commvq_store_pages(commvq_handle *handle, const commvq_pages *page
  *   workspace            >= commvq_tree_workspace_bytes(...) bytes, 256-byte aligned, contents undefined after
  * All data pointers are 16-byte aligned, strides multiples of 8 elements.  Distances between any two positions of a sequence (node or
  * token, on one axis) must not exceed max_position; beyond, rotations are wrong, but nothing faults.  position_free handles turn nothing.
- * bf16 queries with bf16 codebooks: decoded and turned keys, turned queries, softmax weights and decoded values are rounded to
- * bf16 before the products (as a bf16 cache would hold them), all sums are fp32; any other types: fp32 throughout.
+ * bf16 queries with bf16 codebooks: turned queries and keys, softmax weights and values enter the products as fp16 times powers of
+ * two of the rows and codebooks (long contexts, with tables) or as two bf16 parts each (short ones); all sums are fp32, so that the
+ * result is that of fp32 arithmetic rounded to bf16, up to a fraction of that rounding.  Any other types: fp32 throughout.
+ * Codewords that the tokens select must be finite; what the others hold does not matter.
  * COMMVQ_ERR_CONFIG for paired keys and binary values.  Bit-reproducible; concurrent calls need distinct workspaces.
  */
 commvq_status commvq_tree_workspace_bytes(const commvq_handle *handle, int32_t batch, int32_t total_nodes, int32_t max_nodes,
@@ -431,8 +435,8 @@ commvq_status commvq_tree_attn(commvq_handle *handle, const commvq_pages *pages,
                                const void *tables, void *out, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
- * One-time copy of a layer's static codebooks in the order in which commvq_tree_attn streams them: `tables` is a device buffer
- * of commvq_tree_table_bytes() bytes, 16-byte aligned, made anew whenever the codebooks change.  bf16 codebooks (COMMVQ_ERR_CONFIG
+ * One-time copy of a layer's static codebooks in the order in which commvq_tree_attn streams them, and of the powers of two that
+ * bring a head's decoded vectors into fp16's range: `tables` is a device buffer of commvq_tree_table_bytes() bytes, 16-byte aligned, made anew whenever the codebooks change.  bf16 codebooks (COMMVQ_ERR_CONFIG
  * for fp32 ones: their rows are gathered, pass NULL).  Nothing is remembered: calls get `tables` beside the codebooks,
  * which short contexts go on reading.
  */

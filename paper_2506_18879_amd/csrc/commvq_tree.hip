@@ -33,6 +33,7 @@ struct TreeArgs {
     float *part;                      // [row][splits][d] unnormalised
     float2 *stat;                     // [row][splits] (maximum in powers of 2, sum)
     void *out;
+    const float *scales;              // [head] (keys', values' power of two), behind the streamed codebooks
     unsigned axes[4];                 // axis of sub-space j: bits 2 (j % 16) of word j / 16
     long long q_stride, node_stride;
     int batch, Hq, Hkv, G, Mk, Mv, n_hi, n_axes;
@@ -81,7 +82,52 @@ __device__ __forceinline__ unsigned pack_bf16(float lo, float hi)
     return __builtin_bit_cast(unsigned, p);
 }
 
-// 4 bf16 of column l % 16 out of a 4 x 16 block of rows that the 16 lanes around l point at, 8 bytes each, row by row
+// Two fp32 numbers as two bf16 parts each: what is nearest, and what is left of it.  (Of an infinity nothing is left, not a NaN.)
+__device__ __forceinline__ uint2_t split_bf16(float lo, float hi)
+{
+    const unsigned top = pack_bf16(lo, hi);
+    const float x = lo - bf16_lo(top), y = hi - bf16_hi(top);
+    return uint2_t{top, pack_bf16(x == x ? x : 0.f, y == y ? y : 0.f)};
+}
+// acc + (a + al)(b + bl), without the product of the small parts
+__device__ __forceinline__ floatx4_t product(uint4_t a, uint4_t al, uint4_t b, uint4_t bl, floatx4_t acc)
+{
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, al), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, bl), acc, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+}
+
+// The maximum over lanes l, l ^ 16, l ^ 32 and l ^ 48.
+__device__ __forceinline__ float quads_max(float v)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, v);
+    auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const unsigned a0 = a[0], a1 = a[1], w = __builtin_bit_cast(unsigned, fmaxf(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1)));
+    auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+    const unsigned b0 = b[0], b1 = b[1];
+    return fmaxf(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
+}
+
+// fp16 pairs: what the kernels of long contexts keep keys, values, queries and weights in.  Eleven bits instead of bf16's eight; the range is seen to
+// by powers of two, for keys and values one each per head (the codebooks': see k_tree_scale), for queries one per row
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ unsigned pack_f16(float lo, float hi)
+{
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned, __builtin_convertvector(f2{lo, hi}, f16x2_t));  // to nearest, ties to even
+}
+// the power of two that brings the largest of a row's elements to 2^9 .. 2^10 (1 if there is none, or one that is not finite)
+__device__ __forceinline__ float half_scale(float top)
+{
+    if (!(top > 0.f && top < INFINITY)) return 1.f;
+    int e;
+    (void)frexpf(top, &e);
+    return ldexpf(1.f, min(max(10 - e, -100), 100));
+}
+
+// 16-bit elements of column l % 16 out of a 4 x 16 block of rows that the 16 lanes around l point at, 8 bytes each, row by row
 typedef __attribute__((address_space(3))) short4_t *lds_s4_ptr;
 __device__ __forceinline__ uint2_t lds_read_columns(const void *p)
 {
@@ -106,22 +152,23 @@ __device__ __forceinline__ void selection(int lane, uint4_t &sel, unsigned &sidx
 }
 
 // ------------------------------------------------------------------ k_tree_rows
-// One range of a context for 16 NR RG rows of a KV head, 32 tokens at a time.  All eight wavefronts decode four tokens of them each; then NR
-// of them have RG tiles of 16 different rows, 8 / NR of them different elements of the same rows (whose logits each makes by itself).
+// One range of a context for NR tiles of 16 rows of a KV head, 32 tokens at a time.  All eight wavefronts decode four tokens of them each; then
+// 8 / NR of them have a row tile, and different elements of it (whose logits each makes by itself).
 // Decode: the four 16-lane rows of a wavefront hold four codebooks, a lane a 16-byte piece of a codeword; two tokens' pieces
 // are the dense operand of v_smfmac_f32_16x16x64_bf16, whose constant 0/1 operand adds them in fp32 (exactly: products with 1.0).
-// A lane then has four elements of one token, turns them (keys), rounds them to bf16, as a cache of bf16 keys and values
-// would, and leaves them in LDS.  Products: K Q^T with tokens as rows, so that a lane has 4 tokens of one query row; what it
+// A lane then has four elements of one token, turns them (keys), splits each into two bf16 parts (16 bits; the codebooks' range needs bf16's, and
+// one part alone costs a few hundred tokens' result 2^-9 more than its own rounding) and leaves them in LDS.  Queries and weights likewise; of a
+// product's four parts the three that count are added.  Products: K Q^T with tokens as rows, so that a lane has 4 tokens of one query row; what it
 // makes of them is, without any exchange, the operand of V^T P^T, whose other operand is read from LDS by columns.
 // Short contexts are bound by the chain pages -> codes -> rows, so codes are asked for a chunk ahead and a wavefront's rows all at once; longer
 // ones by the codeword rows' way through the L1s, 256 bytes a codebook and token.
 constexpr int kRowsWaves = 8;
 constexpr int kOwn = kChunk / kRowsWaves;       // tokens that a wavefront decodes of a chunk
-template <int NR, int RG, bool AXES>
+template <int NR, bool AXES>
 __global__ __launch_bounds__(64 * kRowsWaves) void k_tree_rows(const TreeArgs a)
 {
     constexpr int ND = kRowsWaves / NR, NX = 8 / ND;                 // wavefronts of a row tile; tiles of 16 elements of a wavefront
-    __shared__ __align__(16) char ktile[kChunk * kRowBytes], vtile[kChunk * kRowBytes];
+    __shared__ __align__(16) char ktile[2][kChunk * kRowBytes], vtile[2][kChunk * kRowBytes];   // high and low parts
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int id = blockIdx.x;
     const int g = id % a.Hkv;
@@ -130,7 +177,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_tree_rows(const TreeArgs a)
     id /= a.row_tiles;
     const int split = id % a.splits, b = id / a.splits;
     const Span s = span_of(a, b);
-    const int R = s.n * a.G, r0 = rt * 16 * NR * RG, t_begin = split * a.split_len, t_end = min(s.L, t_begin + a.split_len);
+    const int R = s.n * a.G, r0 = rt * 16 * NR, t_begin = split * a.split_len, t_end = min(s.L, t_begin + a.split_len);
     if (r0 >= R || t_begin >= t_end) return;
     const int n = lane & 15, gk = lane >> 4, wr = wave / ND, wd = wave % ND;
 
@@ -167,27 +214,27 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_tree_rows(const TreeArgs a)
     auto origin = [&](int ax) { return !AXES || ax == 0 ? t0[0] : ax == 1 ? t0[1] : ax == 2 ? t0[2] : t0[3]; };
 
     // queries, turned and scaled, as second operand: row n, elements 32 ks + 8 gk ..
-    uint4_t qv[RG][4];
+    uint4_t qv[4], ql[4];
+    const int r = r0 + wr * 16 + n;
+    const int node = r / a.G, h = r % a.G;
+    const bool there = r < R;
+    const size_t at = (size_t)(s.n0 + (there ? node : 0)) * a.q_stride + (size_t)(g * a.G + h) * kD;
+    const int32_t *pos = a.node_pos + (size_t)(s.n0 + (there ? node : 0)) * a.n_axes;
 #pragma unroll
-    for (int rg = 0; rg < RG; ++rg) {
-        const int r = r0 + (wr * RG + rg) * 16 + n;
-        const int node = r / a.G, h = r % a.G;
-        const bool there = r < R;
-        const size_t at = (size_t)(s.n0 + (there ? node : 0)) * a.q_stride + (size_t)(g * a.G + h) * kD;
-        const int32_t *pos = a.node_pos + (size_t)(s.n0 + (there ? node : 0)) * a.n_axes;
+    for (int ks = 0; ks < 4; ++ks) {
+        const uint4_t raw = *reinterpret_cast<const uint4_t *>(static_cast<const uint16_t *>(a.q) + at + 32 * ks + 8 * gk);
+        uint4_t w, x;
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            const uint4_t raw = *reinterpret_cast<const uint4_t *>(static_cast<const uint16_t *>(a.q) + at + 32 * ks + 8 * gk);
-            uint4_t w;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int j = 16 * ks + 4 * gk + u, ax = AXES ? axis_of(a, j) : 0;
-                float2 z = make_float2(bf16_lo(raw[u]), bf16_hi(raw[u]));
-                if (a.turn) z = times(z, turned_by(a, pos[ax] - origin(ax), j));
-                w[u] = there ? pack_bf16(z.x * a.scale2, z.y * a.scale2) : 0u;
-            }
-            qv[rg][ks] = w;
+        for (int u = 0; u < 4; ++u) {
+            const int j = 16 * ks + 4 * gk + u, ax = AXES ? axis_of(a, j) : 0;
+            float2 z = make_float2(bf16_lo(raw[u]), bf16_hi(raw[u]));
+            if (a.turn) z = times(z, turned_by(a, pos[ax] - origin(ax), j));
+            const uint2_t p = split_bf16(there ? z.x * a.scale2 : 0.f, there ? z.y * a.scale2 : 0.f);
+            w[u] = p[0];
+            x[u] = p[1];
         }
+        qv[ks] = w;
+        ql[ks] = x;
     }
 
     uint4_t sel;
@@ -199,15 +246,10 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_tree_rows(const TreeArgs a)
     const __amdgpu_buffer_rsrc_t vrows = make_rsrc(static_cast<const uint16_t *>(a.val_cb) + (size_t)g * a.Mv * kK * kD, (unsigned)(a.Mv * kK * kD * 2));
     const unsigned lane_at = (unsigned)(4 * gk) * (kK * kD * 2) + (unsigned)n * 16u;
 
-    floatx4_t o[RG][NX];                             // element 16 (wd NX + x) + 4 gk + i of row n
-    float m[RG], l[RG];
+    floatx4_t o[NX];                                 // element 16 (wd NX + x) + 4 gk + i of row n
+    float m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int rg = 0; rg < RG; ++rg) {
-        m[rg] = -INFINITY;
-        l[rg] = 0.f;
-#pragma unroll
-        for (int x = 0; x < NX; ++x) o[rg][x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int x = 0; x < NX; ++x) o[x] = floatx4_t{0.f, 0.f, 0.f, 0.f};
     // the sums of two tokens, by 16 codebooks
     auto fetch = [&](const __amdgpu_buffer_rsrc_t rows, unsigned code, int blk, uint4_t (&v)[4]) __attribute__((always_inline)) {
 #pragma unroll
@@ -262,82 +304,82 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_tree_rows(const TreeArgs a)
 #pragma unroll
         for (int p = 0; p < kOwn / 2; ++p) {
             const float2 z0 = times(make_float2(acc[p][0], acc[p][1]), e[p][0]), z1 = times(make_float2(acc[p][2], acc[p][3]), e[p][1]);
-            *reinterpret_cast<uint2_t *>(ktile + (wave * kOwn + 2 * p + second) * kRowBytes + n * 16 + half * 8) = uint2_t{pack_bf16(z0.x, z0.y), pack_bf16(z1.x, z1.y)};
+            const uint2_t x = split_bf16(z0.x, z0.y), y = split_bf16(z1.x, z1.y);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) *reinterpret_cast<uint2_t *>(ktile[k] + (wave * kOwn + 2 * p + second) * kRowBytes + n * 16 + half * 8) = uint2_t{x[k], y[k]};
         }
         decode(vrows, cv, a.Mv, acc);
 #pragma unroll
         for (int p = 0; p < kOwn / 2; ++p) {
             const int mine = wave * kOwn + 2 * p + second;
             const bool counts = seen >> mine & 1u;   // (a weight of zero does not hide an infinity)
-            *reinterpret_cast<uint2_t *>(vtile + mine * kRowBytes + n * 16 + half * 8) =
-                uint2_t{counts ? pack_bf16(acc[p][0], acc[p][1]) : 0u, counts ? pack_bf16(acc[p][2], acc[p][3]) : 0u};
+            const uint2_t x = split_bf16(acc[p][0], acc[p][1]), y = split_bf16(acc[p][2], acc[p][3]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) *reinterpret_cast<uint2_t *>(vtile[k] + mine * kRowBytes + n * 16 + half * 8) = uint2_t{counts ? x[k] : 0u, counts ? y[k] : 0u};
         }
         __syncthreads();
-        floatx4_t sc[RG][2];
-#pragma unroll
-        for (int rg = 0; rg < RG; ++rg) sc[rg][0] = sc[rg][1] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+        floatx4_t sc[2];
+        sc[0] = sc[1] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const uint4_t kv = *reinterpret_cast<const uint4_t *>(ktile + (16 * t + n) * kRowBytes + 64 * ks + 16 * gk);
-#pragma unroll
-                for (int rg = 0; rg < RG; ++rg)
-                    sc[rg][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kv), __builtin_bit_cast(bf16x8_t, qv[rg][ks]), sc[rg][t], 0, 0, 0);
+                const uint4_t kv = *reinterpret_cast<const uint4_t *>(ktile[0] + (16 * t + n) * kRowBytes + 64 * ks + 16 * gk);
+                const uint4_t kl = *reinterpret_cast<const uint4_t *>(ktile[1] + (16 * t + n) * kRowBytes + 64 * ks + 16 * gk);
+                sc[t] = product(kv, kl, qv[ks], ql[ks], sc[t]);
             }
-        uint4_t pv[RG];
+        uint4_t pv, pl;
+        float top = -INFINITY;
 #pragma unroll
-        for (int rg = 0; rg < RG; ++rg) {
-            float top = -INFINITY;
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int i = 0; i < 4; ++i) {
+                sc[t][i] = seen >> (16 * t + 4 * gk + i) & 1u ? sc[t][i] : -INFINITY;
+                top = fmaxf(top, sc[t][i]);
+            }
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float now = fmaxf(m, top), base = now == -INFINITY ? 0.f : now;
+        const float old = __builtin_amdgcn_exp2f(m - base);
+        m = now;
+        float sum = 0.f, w[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    sc[rg][t][i] = seen >> (16 * t + 4 * gk + i) & 1u ? sc[rg][t][i] : -INFINITY;
-                    top = fmaxf(top, sc[rg][t][i]);
-                }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float now = fmaxf(m[rg], top), base = now == -INFINITY ? 0.f : now;
-            const float old = __builtin_amdgcn_exp2f(m[rg] - base);
-            m[rg] = now;
-            float sum = 0.f, w[8];
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int i = 0; i < 4; ++i) {
+                w[4 * t + i] = __builtin_amdgcn_exp2f(sc[t][i] - base);
+                sum += w[4 * t + i];
+            }
+        l = l * old + sum;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    w[4 * t + i] = __builtin_amdgcn_exp2f(sc[rg][t][i] - base);
-                    sum += w[4 * t + i];
-                }
-            l[rg] = l[rg] * old + sum;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) pv[rg][i] = pack_bf16(w[2 * i], w[2 * i + 1]);
-#pragma unroll
-            for (int x = 0; x < NX; ++x) o[rg][x] *= old;
+        for (int i = 0; i < 4; ++i) {
+            const uint2_t x = split_bf16(w[2 * i], w[2 * i + 1]);
+            pv[i] = x[0];
+            pl[i] = x[1];
         }
 #pragma unroll
-        for (int x = 0; x < NX; ++x) {
-            const char *at = vtile + (4 * gk + n / 4) * kRowBytes + 32 * (wd * NX + x) + 8 * (n & 3);
-            const uint2_t v0 = lds_read_columns(at), v1 = lds_read_columns(at + 16 * kRowBytes);
-            const uint4_t vv = {v0[0], v0[1], v1[0], v1[1]};
+        for (int x = 0; x < NX; ++x) o[x] *= old;
 #pragma unroll
-            for (int rg = 0; rg < RG; ++rg)
-                o[rg][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vv), __builtin_bit_cast(bf16x8_t, pv[rg]), o[rg][x], 0, 0, 0);
+        for (int x = 0; x < NX; ++x) {
+            uint4_t vv[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const char *at = vtile[k] + (4 * gk + n / 4) * kRowBytes + 32 * (wd * NX + x) + 8 * (n & 3);
+                const uint2_t v0 = lds_read_columns(at), v1 = lds_read_columns(at + 16 * kRowBytes);
+                vv[k] = uint4_t{v0[0], v0[1], v1[0], v1[1]};
+            }
+            o[x] = product(vv[0], vv[1], pv, pl, o[x]);
         }
         if (c0 + kChunk < t_end) __syncthreads();
     }
+    float sum = l;
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (r >= R) return;
+    const size_t row = ((size_t)(s.n0 + r / a.G) * a.Hq + g * a.G + r % a.G) * a.splits + split;
 #pragma unroll
-    for (int rg = 0; rg < RG; ++rg) {
-        float sum = l[rg];
-        sum += __shfl_xor(sum, 16);
-        sum += __shfl_xor(sum, 32);
-        const int r = r0 + (wr * RG + rg) * 16 + n;
-        if (r >= R) continue;
-        const size_t row = ((size_t)(s.n0 + r / a.G) * a.Hq + g * a.G + r % a.G) * a.splits + split;
-#pragma unroll
-        for (int x = 0; x < NX; ++x) *reinterpret_cast<floatx4_t *>(a.part + row * kD + 16 * (wd * NX + x) + 4 * gk) = o[rg][x];
-        if (gk == 0 && wd == 0) a.stat[row] = make_float2(m[rg], sum);
-    }
+    for (int x = 0; x < NX; ++x) *reinterpret_cast<floatx4_t *>(a.part + row * kD + 16 * (wd * NX + x) + 4 * gk) = o[x];
+    if (gk == 0 && wd == 0) a.stat[row] = make_float2(m, sum);
 }
 
 // ------------------------------------------------------------------ k_tree_rows_f32
@@ -611,15 +653,47 @@ __global__ __launch_bounds__(256) void k_tree_pack(const uint4 *__restrict__ cb,
     packed[(((g * 16 + sl) * (M / 16) + m / 16) * kK + word) * 16 + m % 16] = cb[t];
 }
 
+// The power of two that brings sums of M codewords of a head to at most 2^14, so that turned keys (sqrt 2 more) and values fit fp16 whatever the codes
+// and keep its 11 bits down to 2^-28 of that.  A workgroup per (head, codebook kind); numbers that are not finite do not count.
+__global__ __launch_bounds__(1024) void k_tree_scale(const uint4 *__restrict__ cb, float *__restrict__ scales, int M)
+{
+    __shared__ float waves[16];
+    const int n = M * kK * kD / 8;
+    const uint4 *from = cb + (size_t)blockIdx.x * n;
+    float top = 0.f;
+    for (int i = threadIdx.x; i < n; i += 1024) {
+        const uint4 v = from[i];
+        const unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float a = fabsf(bf16_lo(w[k])), b = fabsf(bf16_hi(w[k]));
+            top = fmaxf(top, a < INFINITY ? a : 0.f);
+            top = fmaxf(top, b < INFINITY ? b : 0.f);
+        }
+    }
+    top = wave_max(top);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < 16; ++w) top = fmaxf(top, waves[w]);
+    int e = 0;
+    if (top > 0.f) (void)frexpf(top, &e);            // top < 2^e
+    int m = 0;
+    while (1 << m < M) ++m;
+    scales[2 * blockIdx.x] = ldexpf(1.f, min(max(14 - e - m, -100), 100));
+}
+
 // ------------------------------------------------------------------ host side
 struct TreePlan {
-    int nr, rg;          // rows gathered: wavefronts and row tiles of a wavefront; streamed: sets, 0; decoded ahead: wavefronts of different rows, sets
+    int nr;              // rows gathered: row tiles of a workgroup; streamed: sets of a tile; decoded ahead: wavefronts of different rows
+    int sets;            // decoded ahead: sets of a tile
     int row_tiles, splits, split_len;
     int tiles_per_head;  // decoded ahead: row tiles of 16 of all sequences
     int pass_tiles, passes;  // decoded ahead: token tiles of a pass
-    size_t stat_at, q_at, keys_at, vals_at, seen_at, phases_at, bytes;
+    size_t stat_at, q_at, q_scales_at, keys_at, vals_at, seen_at, phases_at, bytes;
 };
 
+inline size_t tree_packed_bytes(const commvq_config &c) { return (size_t)c.n_kv_heads * (c.m_key + c.m_val) * kK * kD * 2; }
 inline bool wide(const commvq_config &c) { return c.q_dtype != COMMVQ_BF16 || c.codebook_dtype != COMMVQ_BF16; }
 
 void tree_room(const commvq_handle *h, int batch, int total_nodes, bool stream, TreePlan &p)
@@ -631,16 +705,15 @@ void tree_room(const commvq_handle *h, int batch, int total_nodes, bool stream, 
     p.bytes = std::max<size_t>(256, stream ? p.q_at + (size_t)p.tiles_per_head * h->cfg.n_kv_heads * 4096 : p.q_at);
 }
 
-// Rows of a workgroup: the smallest of 16, 32, 64, 128 and 256 that holds the largest tree's.  Ranges: in whole chunks, as many as give
+// Rows of a workgroup: the smallest of 16, 32, 64 and 128 that holds the largest tree's, or 128.  Ranges: in whole chunks, as many as give
 // every compute unit four workgroups.
 TreePlan rows_plan(const commvq_handle *h, int batch, int total_nodes, int max_nodes, int max_seqlen)
 {
     TreePlan p{};
     const int rows = max_nodes * h->G;
     p.nr = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 ? 4 : 8;
-    p.rg = rows > 128 ? 2 : 1;
-    if (wide(h->cfg)) { p.nr = 4; p.rg = 1; }
-    p.row_tiles = (rows + 16 * p.nr * p.rg - 1) / (16 * p.nr * p.rg);
+    if (wide(h->cfg)) p.nr = 4;
+    p.row_tiles = (rows + 16 * p.nr - 1) / (16 * p.nr);
     const int chunk = wide(h->cfg) ? kWideChunk : kChunk;
     const int64_t units = (int64_t)batch * h->cfg.n_kv_heads * p.row_tiles;
     const int64_t chunks = (max_seqlen + chunk - 1) / chunk;
@@ -653,7 +726,7 @@ TreePlan rows_plan(const commvq_handle *h, int batch, int total_nodes, int max_n
 }
 
 // Tiles and ranges of k_tree_stream: of the tile sizes the one, and of whole tiles so many a workgroup, that the last round of workgroups (one
-// per compute unit) ends soonest.  A stage of 512, 1024 and 2048 tokens takes 0.9, 1.2 and 2.0 us (the first two wait for the transfer of the
+// per compute unit) ends soonest, of the sixteen lowest numbers of rounds.  A stage of 512, 1024 and 2048 tokens takes 0.9, 1.2 and 2.0 us (the first two wait for the transfer of the
 // next one): 16 codebooks each, 8 heads, whole calls with tiles of 512 | 1024 | 2048: 16 000 tokens 42.5 | 45.8 | 70.0 us, 32 768 77.9 | 51.4 | 73.2,
 // 65 536 146 | 99.1 | 83.5.
 TreePlan stream_plan(const commvq_handle *h, int batch, int total_nodes, int max_seqlen)
@@ -665,7 +738,8 @@ TreePlan stream_plan(const commvq_handle *h, int batch, int total_nodes, int max
     for (int sets = kStreamMaxSets; sets >= 2; sets /= 2) {
         const int64_t tiles = (max_seqlen + stream_tile(sets) - 1) / stream_tile(sets);
         const double tile_us = (h->cfg.m_key + h->cfg.m_val) * (sets == 8 ? 2.0 : sets == 4 ? 1.2 : 0.9);
-        for (int64_t x = 1; x <= tiles; ++x) {
+        for (int64_t rounds = (units + 255) / 256, last = rounds + 16; rounds < last; ++rounds) {
+            const int64_t most = std::min(256 * rounds / units, tiles), x = (tiles + most - 1) / most;   // ranges of a sequence, tiles of a range
             const double cost = (double)((units * ((tiles + x - 1) / x) + 255) / 256) * (x * tile_us + 3.0);
             if (p.nr == 0 || cost < best) {
                 best = cost;
@@ -691,20 +765,21 @@ TreePlan dense_plan(const commvq_handle *h, int batch, int total_nodes, int max_
     // tiles of 1024 tokens instead of 2048 where that saves rounds of workgroups: 0.62 of a large one's time (8 heads, 8 nodes, 16 codebooks, 1024 | 2048:
     // 8000 tokens 53.8 | 59.3 us, 32 768 104.9 | 85.4; 32 sequences of 600 118.6 | 173.0, of 1500 204.6 | 174.3)
     auto rounds = [&](int sets) { return ((int64_t)batch * ((max_seqlen + sets * kDecodeSetTokens - 1) / (sets * kDecodeSetTokens)) * Hkv * 2 + 255) / 256; };
-    p.rg = 0.62 * (double)rounds(2) < (double)rounds(4) ? 2 : 4;
-    const int tile = p.rg * kDecodeSetTokens, halves = p.rg * kDecodeWaves / kDenseSteps, tiles = (max_seqlen + tile - 1) / tile;
+    p.sets = 0.62 * (double)rounds(2) < (double)rounds(4) ? 2 : 4;
+    const int tile = p.sets * kDecodeSetTokens, halves = p.sets * kDecodeWaves / kDenseSteps, tiles = (max_seqlen + tile - 1) / tile;
     const int64_t all = (int64_t)batch * tiles;
-    p.pass_tiles = (int)std::min<int64_t>(all, std::max(1, kDenseTileHeads * kDecodeMaxSets / p.rg / Hkv));
+    p.pass_tiles = (int)std::min<int64_t>(all, std::max(1, kDenseTileHeads * kDecodeMaxSets / p.sets / Hkv));
     p.passes = (int)((all + p.pass_tiles - 1) / p.pass_tiles);
     p.split_len = tile;
     p.splits = std::min(tiles, p.pass_tiles) * halves;
     tree_room(h, batch, total_nodes, true, p);
-    const size_t steps = (size_t)p.pass_tiles * Hkv * p.rg * kDecodeWaves;
-    p.keys_at = align_up(p.bytes, 256);
+    const size_t steps = (size_t)p.pass_tiles * Hkv * p.sets * kDecodeWaves;
+    p.q_scales_at = align_up(p.bytes, 256);
+    p.keys_at = align_up(p.q_scales_at + (size_t)p.tiles_per_head * Hkv * 64, 256);
     p.vals_at = p.keys_at + steps * kStepBytes;
     p.seen_at = p.vals_at + steps * kStepBytes;
     p.phases_at = align_up(p.seen_at + steps * 4, 256);
-    p.bytes = p.phases_at + (size_t)p.pass_tiles * p.rg * kDecodeWaves * 16 * 64 * 16;
+    p.bytes = p.phases_at + (size_t)p.pass_tiles * p.sets * kDecodeWaves * 16 * 64 * 16;
     return p;
 }
 
@@ -736,11 +811,11 @@ commvq_status check_tree_sizes(const commvq_handle *h, int32_t batch, int32_t to
     return COMMVQ_OK;
 }
 
-template <int NR, int RG>
+template <int NR>
 hipError_t launch_rows(const TreeArgs &a, dim3 grid, hipStream_t s)
 {
-    if (a.n_axes > 1) k_tree_rows<NR, RG, true><<<grid, 64 * kRowsWaves, 0, s>>>(a);
-    else k_tree_rows<NR, RG, false><<<grid, 64 * kRowsWaves, 0, s>>>(a);
+    if (a.n_axes > 1) k_tree_rows<NR, true><<<grid, 64 * kRowsWaves, 0, s>>>(a);
+    else k_tree_rows<NR, false><<<grid, 64 * kRowsWaves, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -807,8 +882,8 @@ hipError_t launch_dense_as(const TreeArgs &a, const DensePass &d, dim3 grid, hip
 hipError_t launch_dense(const TreeArgs &a, const TreePlan &p, int passes, const char *tables, char *workspace, hipStream_t s)
 {
     DensePass d{workspace + p.keys_at, workspace + p.vals_at, reinterpret_cast<unsigned *>(workspace + p.seen_at),
-                reinterpret_cast<floatx4_t *>(workspace + p.phases_at), reinterpret_cast<uint4_t *>(workspace + p.q_at),
-                p.tiles_per_head, 0, p.pass_tiles, p.rg, p.rg * kDecodeSetTokens, p.rg * kDecodeWaves, 0, (a.max_nodes * a.G + 15) / 16};
+                reinterpret_cast<floatx4_t *>(workspace + p.phases_at), reinterpret_cast<uint4_t *>(workspace + p.q_at), reinterpret_cast<float *>(workspace + p.q_scales_at),
+                p.tiles_per_head, 0, p.pass_tiles, p.sets, p.sets * kDecodeSetTokens, p.sets * kDecodeWaves, 0, (a.max_nodes * a.G + 15) / 16};
     const int64_t turns = ((int64_t)a.batch * a.Hkv * d.turn_tiles + kDecodeWaves - 1) / kDecodeWaves;
     const int64_t decode = 2ll * d.tiles * a.Hkv, dense = (int64_t)d.tiles * a.Hkv * p.row_tiles * (d.steps / kDenseSteps);
     if (std::max(turns + decode, dense) > 0x7fffffff) return hipErrorInvalidValue;
@@ -899,6 +974,7 @@ commvq_status commvq_tree_attn(commvq_handle *h, const commvq_pages *pages, cons
     a.q = q; a.node_k = node_keys; a.node_v = node_vals; a.key_pages = key_pages; a.val_pages = val_pages; a.key_cb = key_cb; a.val_cb = val_cb;
     a.seq_lens = t->seq_lens; a.tables = t->block_tables; a.cu = t->cu_nodes; a.node_pos = t->node_pos; a.key_pos = t->key_pos;
     a.mask = reinterpret_cast<const unsigned long long *>(t->node_mask);
+    if (tables) a.scales = reinterpret_cast<const float *>(static_cast<const char *>(tables) + tree_packed_bytes(c));
     a.tbl_hi = h->tbl_hi; a.tbl_lo = h->tbl_lo;
     a.part = static_cast<float *>(workspace);
     a.stat = reinterpret_cast<float2 *>(static_cast<char *>(workspace) + p.stat_at);
@@ -907,7 +983,7 @@ commvq_status commvq_tree_attn(commvq_handle *h, const commvq_pages *pages, cons
     a.batch = t->batch; a.Hq = c.n_q_heads; a.Hkv = c.n_kv_heads; a.G = h->G; a.Mk = c.m_key; a.Mv = c.m_val; a.n_hi = h->n_hi;
     a.n_axes = pages->n_axes; a.block_bits = __builtin_ctz((unsigned)pages->block_size); a.n_blocks = pages->n_blocks; a.max_blocks = pages->max_blocks;
     a.total_nodes = t->total_nodes; a.max_nodes = t->max_nodes; a.max_seqlen = t->max_seqlen;
-    a.splits = p.splits; a.split_len = p.split_len; a.row_tiles = p.row_tiles; a.halves = way == kDense ? p.rg * kDecodeWaves / kDenseSteps : 1;
+    a.splits = p.splits; a.split_len = p.split_len; a.row_tiles = p.row_tiles; a.halves = way == kDense ? p.sets * kDecodeWaves / kDenseSteps : 1;
     a.turn = !c.position_free; a.q_bf16 = c.q_dtype == COMMVQ_BF16; a.cb_bf16 = c.codebook_dtype == COMMVQ_BF16;
     a.scale2 = h->scale * kLog2e;
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -917,11 +993,10 @@ commvq_status commvq_tree_attn(commvq_handle *h, const commvq_pages *pages, cons
         if (way == kDense) e = launch_dense(a, p, (int)((tiles + p.pass_tiles - 1) / p.pass_tiles), static_cast<const char *>(tables), static_cast<char *>(workspace), s);
         else if (way == kStream) e = launch_stream(a, p.nr, static_cast<const char *>(tables), grid, s);
         else if (wide(c)) e = launch_wide(a, grid, s);
-        else if (p.nr == 1) e = launch_rows<1, 1>(a, grid, s);
-        else if (p.nr == 2) e = launch_rows<2, 1>(a, grid, s);
-        else if (p.nr == 4) e = launch_rows<4, 1>(a, grid, s);
-        else if (p.rg == 1) e = launch_rows<8, 1>(a, grid, s);
-        else e = launch_rows<8, 2>(a, grid, s);
+        else if (p.nr == 1) e = launch_rows<1>(a, grid, s);
+        else if (p.nr == 2) e = launch_rows<2>(a, grid, s);
+        else if (p.nr == 4) e = launch_rows<4>(a, grid, s);
+        else e = launch_rows<8>(a, grid, s);
         if (e != hipSuccess) return COMMVQ_ERR_LAUNCH;
     }
     const dim3 rows((unsigned)((int64_t)t->total_nodes * c.n_q_heads));
@@ -942,7 +1017,7 @@ commvq_status commvq_tree_table_bytes(const commvq_handle *h, size_t *bytes)
     if (!h || !bytes) return COMMVQ_ERR_NULL;
     const commvq_config &c = h->cfg;
     if (c.codebook_dtype != COMMVQ_BF16 || c.key_format != COMMVQ_KEYS_INDEXED || c.value_format != COMMVQ_VALUES_INDEXED) return COMMVQ_ERR_CONFIG;
-    *bytes = (size_t)c.n_kv_heads * (c.m_key + c.m_val) * kK * kD * 2;
+    *bytes = tree_packed_bytes(c) + align_up((size_t)c.n_kv_heads * 8, 256);
     return COMMVQ_OK;
 }
 
@@ -962,6 +1037,11 @@ commvq_status commvq_tree_prepare(commvq_handle *h, const void *key_cb, const vo
     k_tree_pack<<<dim3((unsigned)(kp / 256)), 256, 0, s>>>(static_cast<const uint4 *>(key_cb), to, c.m_key, kp);
     if (hipGetLastError() != hipSuccess) return COMMVQ_ERR_LAUNCH;
     k_tree_pack<<<dim3((unsigned)(vp / 256)), 256, 0, s>>>(static_cast<const uint4 *>(val_cb), to + kp, c.m_val, vp);
+    if (hipGetLastError() != hipSuccess) return COMMVQ_ERR_LAUNCH;
+    float *scales = reinterpret_cast<float *>(static_cast<char *>(tables) + tree_packed_bytes(c));
+    k_tree_scale<<<dim3((unsigned)c.n_kv_heads), 1024, 0, s>>>(static_cast<const uint4 *>(key_cb), scales, c.m_key);
+    if (hipGetLastError() != hipSuccess) return COMMVQ_ERR_LAUNCH;
+    k_tree_scale<<<dim3((unsigned)c.n_kv_heads), 1024, 0, s>>>(static_cast<const uint4 *>(val_cb), scales + 1, c.m_val);
     return hipGetLastError() == hipSuccess ? COMMVQ_OK : COMMVQ_ERR_LAUNCH;
 }
 

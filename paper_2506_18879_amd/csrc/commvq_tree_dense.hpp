@@ -21,6 +21,7 @@ struct DensePass {
     unsigned *seen;
     floatx4_t *phases;   // explicit positions: [tile][step][slice][lane], E of the lane's two sub-spaces
     uint4_t *queries;    // [head][row tile of 16][k-step][lane], see turn_rows
+    float *query_scales; // [head][row tile of 16][16], their powers of two
     int tiles_per_head;  // row tiles of a head, of all sequences
     int tile0, tiles;
     int sets, tile_tokens, steps;  // of a tile: sets of a wavefront, tokens, sets
@@ -30,18 +31,20 @@ struct DensePass {
 // where the row tiles of sequence b begin among those of a KV head
 __host__ __device__ __forceinline__ int first_tile(int n0, int G, int b) { return n0 * G / 16 + b; }
 
-// The sequence and the place in it of tile t of the batch, by one wavefront; false if there are not so many.
+// The sequence and the place in it of tile t of the batch, by one wavefront; false if there are not so many.  (A sequence without nodes has none:
+// nothing reads its tiles, and a first node's position is not there.)
 __device__ __forceinline__ bool find_tile(const TreeArgs &a, int tile_tokens, int t, int lane, int &b, int &at)
 {
     if (a.batch == 1) {
         b = 0;
         at = t;
-        return (long long)t * tile_tokens < min(max(a.seq_lens[0], 0), a.max_seqlen);
+        const Span s = span_of(a, 0);
+        return s.n > 0 && (long long)t * tile_tokens < s.L;
     }
     int before = 0;
     for (int c = 0; c < a.batch; c += 64) {
-        const int L = c + lane < a.batch ? min(max(a.seq_lens[c + lane], 0), a.max_seqlen) : 0;
-        const int own = (L + tile_tokens - 1) / tile_tokens;
+        const Span s = span_of(a, min(c + lane, a.batch - 1));
+        const int own = c + lane < a.batch && s.n > 0 ? (s.L + tile_tokens - 1) / tile_tokens : 0;
         int incl = own;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
@@ -78,7 +81,7 @@ __device__ __forceinline__ int slice_dim(int pair, int gk, int e) { return 16 * 
 // cores add them (selection operand and order of the codebooks as in k_score_stream: no bank conflicts, whatever the codes), a lane gets four
 // elements of one token.  Keys: it turns its two sub-spaces; the wavefront's halves of two slices are exchanged, so that a lane has 4 elements of
 // each half's token n, and leaves them four slices at a time.  Values: two slices of a set go through 1 KiB of LDS, written by token and read by columns (ds_read_b64_tr_b16).
-// Rounded to bf16, as a bf16 cache would hold them.
+// Times the head's power of two, rounded to fp16.
 // EXPLICIT: positions from the pool, or of several axes; the phase factors are k_tree_phases' then.
 template <int NB, int kSets, bool KEYS, bool EXPLICIT>
 __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &d, const char *src, int g, int tile)
@@ -99,6 +102,7 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
         return;
     }
     const Span s = span_of(a, b);
+    const float scale = a.scales[2 * g + (KEYS ? 0 : 1)];
     const int n = lane & 15, gk = lane >> 4, par = gk & 1, second = gk >> 1;
     const int c0 = at * kTile;
 
@@ -193,7 +197,7 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
                 __builtin_amdgcn_s_barrier();
                 order();
                 if (blk == 0) {
-                    e_lo = e_next;
+                    e_lo = e_next * scale;
                     asm volatile("" : "+v"(e_lo));
                     if (FINE && a.turn) e_next = fine((sl + 1) & 15);
                 }
@@ -213,8 +217,8 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
                         for (int u = 0; u < 2; ++u) {
                             float ex, ey;
                             if constexpr (EXPLICIT) {
-                                ex = e_hi[2 * u];
-                                ey = e_hi[2 * u + 1];
+                                ex = e_hi[2 * u] * scale;
+                                ey = e_hi[2 * u + 1] * scale;
                             } else {
                                 ex = e_hi[2 * u] * e_lo[2 * u] - e_hi[2 * u + 1] * e_lo[2 * u + 1];
                                 ey = e_hi[2 * u] * e_lo[2 * u + 1] + e_hi[2 * u + 1] * e_lo[2 * u];
@@ -222,7 +226,7 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
                             w[2 * u] = z[2 * u] * ex + z[2 * u + 1] * ey;
                             w[2 * u + 1] = z[2 * u + 1] * ex - z[2 * u] * ey;
                         }
-                        const uint2_t k = {pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])};
+                        const uint2_t k = {pack_f16(w[0], w[1]), pack_f16(w[2], w[3])};
                         if (i % 2 == 0) {
                             kw[ts] = k;
                             return;
@@ -245,7 +249,8 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
                     } else {
                         if (slot != 1 && slot != 4) return;
                         const int ts = 2 * p + slot / 4;
-                        uint2_t v = {pack_bf16(acc[ts][0], acc[ts][1]), pack_bf16(acc[ts][2], acc[ts][3])};
+                        const floatx4_t z = acc[ts] * scale;
+                        uint2_t v = {pack_f16(z[0], z[1]), pack_f16(z[2], z[3])};
                         // (a weight of zero does not hide an infinity: tokens that do not count are cleared)
                         asm("v_cndmask_b32 %0, 0, %0, %1" : "+v"(v[0]) : "s"(seen[ts]));
                         asm("v_cndmask_b32 %0, 0, %0, %1" : "+v"(v[1]) : "s"(seen[ts]));
@@ -300,8 +305,8 @@ __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                 // the transfer behind the last stage has landed
 }
 
-// Queries of row tile id of the launch's [sequence][row tile][head], turned, scaled and rounded to bf16, by a wavefront: the second operand of the
-// logits, 8 elements of row lane % 16 in the order in which the decoded keys have them.
+// Queries of row tile id of the launch's [sequence][row tile][head], turned, times a power of two of the row and rounded to fp16, by a wavefront: the
+// second operand of the logits, 8 elements of row lane % 16 in the order in which the decoded keys have them.
 __device__ __forceinline__ void turn_rows(const TreeArgs &a, const DensePass &d, int id, int lane)
 {
     const int g = id % a.Hkv;
@@ -315,19 +320,29 @@ __device__ __forceinline__ void turn_rows(const TreeArgs &a, const DensePass &d,
     const bool there = r < R;
     const int node = s.n0 + (there ? r / a.G : 0);
     const uint16_t *row = static_cast<const uint16_t *>(a.q) + (size_t)node * a.q_stride + (size_t)(g * a.G + r % a.G) * kD;
-    uint4_t *to = d.queries + ((size_t)g * d.tiles_per_head + first_tile(s.n0, a.G, b) + rt) * 256 + lane;
+    const size_t tile = (size_t)g * d.tiles_per_head + first_tile(s.n0, a.G, b) + rt;
+    unsigned raw[4][4];
+    float top = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            raw[ks][u] = *reinterpret_cast<const unsigned *>(row + slice_dim(2 * ks + u / 2, gk, 2 * (u & 1)));
+            top = fmaxf(top, fmaxf(fabsf(bf16_lo(raw[ks][u])), fabsf(bf16_hi(raw[ks][u]))));
+        }
+    const float scale = half_scale(quads_max(top));
+    if (gk == 0) d.query_scales[tile * 16 + n] = scale;
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
         uint4_t w;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int e = slice_dim(2 * ks + u / 2, gk, 2 * (u & 1)), j = e / 2, ax = axis_of(a, j);
-            const unsigned raw = *reinterpret_cast<const unsigned *>(row + e);
-            float2 z = make_float2(bf16_lo(raw), bf16_hi(raw));
+            const int j = slice_dim(2 * ks + u / 2, gk, 2 * (u & 1)) / 2, ax = axis_of(a, j);
+            float2 z = make_float2(bf16_lo(raw[ks][u]) * scale, bf16_hi(raw[ks][u]) * scale);
             if (a.turn) z = times(z, turned_by(a, a.node_pos[(size_t)node * a.n_axes + ax] - a.node_pos[(size_t)s.n0 * a.n_axes + ax], j));
-            w[u] = there ? pack_bf16(z.x * a.scale2, z.y * a.scale2) : 0u;
+            w[u] = there ? pack_f16(z.x, z.y) : 0u;
         }
-        to[64 * ks] = w;
+        d.queries[tile * 256 + 64 * ks + lane] = w;
     }
 }
 
@@ -375,17 +390,6 @@ __global__ __launch_bounds__(kDecodeThreads) void k_tree_decode(const TreeArgs a
     const int tile = id % d.tiles;
     if (id < d.tiles) decode_tile<NBK, SETS, true, EXPLICIT>(a, d, packed + (size_t)g * 16 * NBK * kStageBytes, g, tile);
     else decode_tile<NBV, SETS, false, false>(a, d, packed + (size_t)(a.Hkv * NBK + g * NBV) * 16 * kStageBytes, g, tile);
-}
-
-// The maximum over lanes l, l ^ 16, l ^ 32 and l ^ 48.
-__device__ __forceinline__ float quads_max(float v)
-{
-    const unsigned u = __builtin_bit_cast(unsigned, v);
-    auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    const unsigned a0 = a[0], a1 = a[1], w = __builtin_bit_cast(unsigned, fmaxf(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1)));
-    auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
-    const unsigned b0 = b[0], b1 = b[1];
-    return fmaxf(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
 }
 
 // ------------------------------------------------------------------ k_tree_dense
@@ -445,11 +449,15 @@ __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs 
         return;
     }
     const int tiles16 = (R + 15) / 16;
+    const float head_unit = a.scale2 / a.scales[2 * g], undo = 1.f / a.scales[2 * g + 1];   // of the logits (and of a row's), of the values
+    float unit[RT];
 
     uint4_t qv[RT][4];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const uint4_t *from = d.queries + ((size_t)g * d.tiles_per_head + first_tile(s.n0, a.G, b) + min(r0 / 16 + rt, tiles16 - 1)) * 256 + lane;
+        const size_t tile16 = (size_t)g * d.tiles_per_head + first_tile(s.n0, a.G, b) + min(r0 / 16 + rt, tiles16 - 1);
+        const uint4_t *from = d.queries + tile16 * 256 + lane;
+        unit[rt] = head_unit / d.query_scales[tile16 * 16 + n];
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) qv[rt][ks] = from[64 * ks];   // (rows past the last take the last tile's and are not written)
     }
@@ -473,7 +481,7 @@ __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs 
     if constexpr (!SHARED) load_keys(kp + (size_t)wt * kStepBytes);
     unsigned seen = d.seen[step0 + wt];
     if constexpr (SHARED) {                                          // (from here on the transfers are all that is counted)
-        asm volatile("" ::"v"(qv[0][0]), "v"(qv[RT - 1][3]), "s"(seen));
+        asm volatile("" ::"v"(qv[0][0]), "v"(qv[RT - 1][3]), "v"(unit[0]), "v"(unit[RT - 1]), "s"(seen));
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
     for (int st = wt, round = 0; st < STEPS; st += WT, ++round) {
@@ -501,7 +509,7 @@ __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs 
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
-                    sc[rt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kv[h][ks]), __builtin_bit_cast(bf16x8_t, qv[rt][ks]), sc[rt][h], 0, 0, 0);
+                    sc[rt][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, kv[h][ks]), __builtin_bit_cast(f16x8_t, qv[rt][ks]), sc[rt][h], 0, 0, 0);
             }
         const unsigned now_seen = seen;
         const int next = min(st + WT, STEPS - 1);                    // (behind the last step: once more, not used)
@@ -524,17 +532,17 @@ __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs 
         uint4_t pv[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            // weights are relative to a number that is raised to the maximum only when a logit is more than 2^8 above it: rarely after the first
-            // steps, and neither sums nor weights (bf16: relative) care for a factor of 256
+            // Weights are relative to a number that is raised, to 2^7 below the maximum, only when a logit is more than 2^15 above it: rarely after
+            // the first steps.  They stay below fp16's 65504, and its smallest number is 2^-31 of the largest weight or less.
             float top = -INFINITY;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[rt][h][i]);
-            if (__ballot(top > m[rt] + 8.f)) {
-                top = quads_max(top);
-                const float now = fmaxf(m[rt], top), old = __builtin_amdgcn_exp2f(m[rt] - now);   // (a lane without any: -inf - -inf, not used)
-                const float f = m[rt] == -INFINITY ? 0.f : old;
+            top *= unit[rt];
+            if (__ballot(top > m[rt] + 15.f)) {
+                const float now = fmaxf(m[rt], quads_max(top) - 7.f);
+                const float f = m[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[rt] - now);
                 m[rt] = now;
                 l[rt] *= f;
 #pragma unroll
@@ -544,24 +552,26 @@ __global__ __launch_bounds__(64 * kDenseWaves) void k_tree_dense(const TreeArgs 
             float w[8], sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                w[i] = __builtin_amdgcn_exp2f(sc[rt][i / 4][i & 3] - base);
+                w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rt][i / 4][i & 3], unit[rt], -base));
                 sum += w[i];
             }
             l[rt] += sum;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) pv[rt][i] = pack_bf16(w[2 * i], w[2 * i + 1]);
+            for (int i = 0; i < 4; ++i) pv[rt][i] = pack_f16(w[2 * i], w[2 * i + 1]);
         }
 #pragma unroll
         for (int x = 0; x < 8; ++x)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
-                o[rt][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vv[x]), __builtin_bit_cast(bf16x8_t, pv[rt]), o[rt][x], 0, 0, 0);
+                o[rt][x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, vv[x]), __builtin_bit_cast(f16x8_t, pv[rt]), o[rt][x], 0, 0, 0);
     }
     if constexpr (SHARED) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the transfers behind the last round have landed
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         l[rt] += __shfl_xor(l[rt], 16);
         l[rt] += __shfl_xor(l[rt], 32);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) o[rt][x] *= undo;
     }
     // where the rows' parts go; what a pass before has left there is asked for before the wavefronts meet
     float *to[RT];

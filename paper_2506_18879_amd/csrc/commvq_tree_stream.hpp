@@ -11,12 +11,14 @@ constexpr int stream_tile(int sets) { return 32 * kStreamWaves * sets; }   // 64
 constexpr int kStreamMaxTile = stream_tile(kStreamMaxSets);
 // LDS behind the two stages.  Key stages: coarse phase factors of the tile [33 rows][64], row maxima [8 wavefronts][16], slots [set][wavefront][32];
 // value stages, over the phase factors: per wavefront 1 KiB for one set's values on their way to columns, then for its sums of 16 elements [lane][4].
-// All stages: the queries [pair of slices][lane][4 bf16].
+// All stages: the queries [pair of slices][lane][4 fp16].
 constexpr int kMaxAt = kAuxAt + (kStreamMaxTile / kLo + 1) * kJ * 8;
 constexpr int kSlotAt = kMaxAt + kStreamWaves * kStreamRows * 4;
 constexpr int kQueryAt = kSlotAt + kStreamMaxTile * 4;
 constexpr int kTreeLds = kQueryAt + 8 * 64 * 8;
 static_assert(kTreeLds <= kLdsBytes && kStreamWaves * 1024 <= kMaxAt - kAuxAt, "fits a compute unit");
+
+constexpr float kShift = 14.f;                                       // largest weight: 2^14
 
 typedef __attribute__((address_space(3))) const uint2_t *tree_u2_ptr;
 typedef __attribute__((address_space(3))) floatx4_t *tree_f4_out;
@@ -29,10 +31,10 @@ typedef __attribute__((address_space(3))) floatx4_t *tree_f4_out;
 // apart and share the fine phase factor.
 // Keys, per stage and set: the codes (registers for the whole tile) name 16-byte pieces in LDS, the matrix cores add them
 // (selection operand as in k_score_stream, whose rule for the order of the codebooks keeps the reads free of bank conflicts), the lane turns its two
-// sub-spaces and rounds to bf16.  After two slices, an exchange of the wavefront's halves makes them the operand of
+// sub-spaces, times the head's power of two, and rounds to fp16.  After two slices, an exchange of the wavefront's halves makes them the operand of
 // logits (tokens as rows) += K Q^T (16x16x16: the faster 16x16x32 would keep four slices in registers).
 // Softmax: the workgroup's maxima meet in LDS, so that all wavefronts' weights are relative to the same number; weights stay in
-// registers as bf16 operands for all value stages.
+// registers as fp16 operands for all value stages (2^14 for the largest: below 65504, and the smallest number is 2^-38 of it).
 // Values, per pair of slices: the sums of a set go through 1 KiB of LDS, written by token and read by columns
 // (ds_read_b64_tr_b16), into sums for 16 elements += V^T P^T; these meet in LDS across the wavefronts and are added to the rows' parts
 // in memory (the range's earlier tiles, scaled to the new maximum).
@@ -50,6 +52,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a
     const int R = s.n * a.G, t_begin = split * a.split_len, t_end = min(s.L, t_begin + a.split_len);
     if (R < 1 || t_begin >= t_end) return;
     const int n = lane & 15, gk = lane >> 4, par = gk & 1, second = gk >> 1;
+    const float scale = a.scales[2 * g], head_unit = a.scale2 / scale, val_scale = a.scales[2 * g + 1], undo = 1.f / val_scale;
     const int t0 = a.turn ? a.node_pos[(size_t)s.n0 * a.n_axes] : 0;
 
     const char *ksrc = packed + (size_t)g * 16 * NBK * kStageBytes;
@@ -77,18 +80,29 @@ __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a
     const int32_t *table = a.tables + (size_t)b * a.max_blocks;
     const int in_page = (1 << a.block_bits) - 1;
     float m = -INFINITY, l = 0.f;
-    // queries, turned, scaled and rounded to bf16: wavefront w those of pair of slices w, 4 elements of row n in the order of the keys
+    // queries, turned, times a power of two and rounded to fp16: wavefront w those of pair of slices w, 4 elements of row n in the order of the keys
+    float unit;                                               // of row n's logits
     {
         const bool there = n < R;
         const int node = s.n0 + (there ? n / a.G : 0);
         const int e = slice_dim(wave, gk, 0);
         const uint2_t raw = *reinterpret_cast<const uint2_t *>(static_cast<const uint16_t *>(a.q) + (size_t)node * a.q_stride + (size_t)(g * a.G + n % a.G) * kD + e);
+        // (the power of two is the row's: the wavefronts' maxima meet)
+        float *maxima = reinterpret_cast<float *>(lds + kMaxAt);
+        const float top = quads_max(fmaxf(fmaxf(fabsf(bf16_lo(raw[0])), fabsf(bf16_hi(raw[0]))), fmaxf(fabsf(bf16_lo(raw[1])), fabsf(bf16_hi(raw[1])))));
+        if (gk == 0) maxima[wave * 16 + n] = top;
+        __syncthreads();
+        float all = 0.f;
+#pragma unroll
+        for (int w = 0; w < kStreamWaves; ++w) all = fmaxf(all, maxima[w * 16 + n]);
+        const float q_scale = half_scale(all);
+        unit = head_unit / q_scale;
         uint2_t w;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            float2 z = make_float2(bf16_lo(raw[u]), bf16_hi(raw[u]));
+            float2 z = make_float2(bf16_lo(raw[u]) * q_scale, bf16_hi(raw[u]) * q_scale);
             if (a.turn) z = times(z, turned_by(a, a.node_pos[(size_t)node * a.n_axes] - t0, e / 2 + u));
-            w[u] = there ? pack_bf16(z.x * a.scale2, z.y * a.scale2) : 0u;
+            w[u] = there ? pack_f16(z.x, z.y) : 0u;
         }
         *reinterpret_cast<uint2_t *>(lds + kQueryAt + (wave * 64 + lane) * 8) = w;
     }
@@ -212,7 +226,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a
                     const int buf = (NBK * i + blk) & 1;
                     stage_begin();
                     if (blk == 0) {
-                        e_lo = e_next;
+                        e_lo = e_next * scale;
                         asm volatile("" : "+v"(e_lo));            // (has arrived: the next stage's transfers are not to be waited for)
                         if (a.turn) e_next = fine((sl + 1) & 15);
                         if (i == 1) qv = *reinterpret_cast<tree_u2_ptr>(kQueryAt + (pr * 64 + lane) * 8);
@@ -234,7 +248,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a
                                   w[2 * u] = z[2 * u] * ex + z[2 * u + 1] * ey;
                                   w[2 * u + 1] = z[2 * u + 1] * ex - z[2 * u] * ey;
                               }
-                              const uint2_t k = {pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])};
+                              const uint2_t k = {pack_f16(w[0], w[1]), pack_f16(w[2], w[3])};
                               if (i == 0) {
                                   kw[ts] = k;
                                   return;
@@ -246,8 +260,8 @@ __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a
                                   ka[r] = x[0];
                                   kb[r] = x[1];
                               }
-                              sc[ts][0] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4_t, ka), __builtin_bit_cast(short4_t, qv), sc[ts][0], 0, 0, 0);
-                              sc[ts][1] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4_t, kb), __builtin_bit_cast(short4_t, qv), sc[ts][1], 0, 0, 0);
+                              sc[ts][0] = __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4_t, ka), __builtin_bit_cast(f16x4_t, qv), sc[ts][0], 0, 0, 0);
+                              sc[ts][1] = __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4_t, kb), __builtin_bit_cast(f16x4_t, qv), sc[ts][1], 0, 0, 0);
                           });
                 }
             }
@@ -285,7 +299,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a
                     for (int i = 0; i < 4; ++i) top = fmaxf(top, sc[ts][h][i]);
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            if (gk == 0) maxima[wave * 16 + n] = top;
+            if (gk == 0) maxima[wave * 16 + n] = top * unit;
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -295,7 +309,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a
             float now = m;
 #pragma unroll
             for (int w = 0; w < kStreamWaves; ++w) now = fmaxf(now, maxima[w * 16 + n]);
-            const float base = now == -INFINITY ? 0.f : now;
+            const float base = now == -INFINITY ? 0.f : now, ref = base - kShift;
             l *= __builtin_amdgcn_exp2f(m - base);
             m = now;
 #pragma unroll
@@ -305,11 +319,11 @@ __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a
                     float w[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        w[i] = __builtin_amdgcn_exp2f(sc[ts][h][i] - base);
+                        w[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[ts][h][i], unit, -ref));
                         l += w[i];
                     }
-                    pv[ts][2 * h] = pack_bf16(w[0], w[1]);
-                    pv[ts][2 * h + 1] = pack_bf16(w[2], w[3]);
+                    pv[ts][2 * h] = pack_f16(w[0], w[1]);
+                    pv[ts][2 * h + 1] = pack_f16(w[2], w[3]);
                 }
         }
         float old = 0.f;                                          // factor of the row's earlier tiles
@@ -332,6 +346,8 @@ __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a
                 t.x += x.x;
                 t.y += x.y;
             }
+            t.x *= undo;
+            t.y *= undo;
             float2 *to = reinterpret_cast<float2 *>(mine + 16 * sp);
             if (c0 > t_begin) { const float2 was = *to; t.x += was.x * old; t.y += was.y * old; }
             *to = t;
@@ -357,7 +373,8 @@ __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a
                               if (blk != NBV - 1) return;
                               if (slot == 1 || slot == 3) {
                                   const int y = slot == 3, ts = 2 * p + y;
-                                  uint2_t v = {pack_bf16(acc[ts][0], acc[ts][1]), pack_bf16(acc[ts][2], acc[ts][3])};
+                                  const floatx4_t z = acc[ts] * val_scale;
+                                  uint2_t v = {pack_f16(z[0], z[1]), pack_f16(z[2], z[3])};
                                   // (a weight of zero does not hide an infinity: tokens that do not count are cleared)
                                   asm("v_cndmask_b32 %0, 0, %0, %1" : "+v"(v[0]) : "s"(seen[ts]));
                                   asm("v_cndmask_b32 %0, 0, %0, %1" : "+v"(v[1]) : "s"(seen[ts]));
@@ -376,7 +393,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a
                               }
                               if (i == 1 && (slot == 4 || slot == 6)) {
                                   const int y = slot == 6, ts = 2 * p + y;
-                                  o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, vv[y]), __builtin_bit_cast(bf16x8_t, pv[ts]), o, 0, 0, 0);
+                                  o = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, vv[y]), __builtin_bit_cast(f16x8_t, pv[ts]), o, 0, 0, 0);
                               }
                           });
                 }
@@ -403,7 +420,7 @@ __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a
         float t = 0.f;
 #pragma unroll
         for (int w = 0; w < kStreamWaves; ++w) t += sums[w * 16 + qr];
-        a.stat[out_row] = make_float2(m_row, t);
+        a.stat[out_row] = make_float2(m_row - kShift, t);
     }
 }
 

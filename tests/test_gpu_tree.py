@@ -1,12 +1,12 @@
 """Attention of drafted trees over a paged cache, against the definition in 64 bits (decode, turn, softmax, sum, row by row of the tables).
 
-Tolerances.  u = eps / 2 is a rounding's largest relative error (bf16: 2^-8).  bf16 results round four times on the way: turned queries and keys
-(both errors enter a logit: Sum_d q_d k_d scale (e_q + e_k), at most 2u Sum_d |q_d k_d| scale =: D), the weights, the values, the
-result.  A normalised weight is then off by at most the factor exp(2 D) (1 + u)^2, an element by (exp(2 D) (1 + u)^3 - 1) Sum p |v| + u |out|:
-that is the bound of every element.  Taken together errors are independent, u / sqrt(3) each in the root mean square if evenly spread: sqrt(2) u / sqrt(3)
-for the logits (which are of unit variance here) and three times u / sqrt(3), sqrt(5/3) u = 1.29 u = 5.0e-3 of the results' norm at most;
-twice that is the bound of the norm.  fp32 results: sums of at most 128 + 32 terms a logit and 2^13 terms a result, 2^-24 each and
-random in sign, stay below 2^-24 (13 * 8 + 91) = 1.2e-5 of the norm, and four times that in any element relative to Sum p |v|."""
+Tolerances.  u = eps / 2 is a rounding's largest relative error.  bf16 results are rounded once to bf16 (u = 2^-8); on the way turned queries and
+keys, weights and values are rounded to fp16 (h = 2^-11) or to two bf16 parts (less).  Errors of queries and keys enter a logit with at most
+2h Sum_d |q_d k_d| scale =: D, a normalised weight is then off by at most the factor exp(2 D) (1 + h)^2 (and 2^-32 of the largest weight a token, less than another
+h for the 70 001 tokens here), an element before its last rounding by E = (exp(2 D) (1 + h)^3 - 1) Sum p |v|, after it by E + u (|out| + E).
+Taken together the errors are independent, u / sqrt(3) and h / sqrt(3) each in the root mean square if evenly spread: sqrt(u^2 + 4 h^2) / sqrt(3) = 2.33e-3 of the
+results' norm (logits are of unit variance here); twice that is the bound of the norm.  fp32 results: sums of at most 128 + 32 terms a logit and 2^13
+terms a result, 2^-24 each and random in sign, stay below 2^-24 (13 * 8 + 91) = 1.2e-5 of the norm, and four times that in any element relative to Sum p |v|."""
 import math
 
 import pytest
@@ -15,7 +15,8 @@ import torch
 import paper_2506_18879_amd as cv
 
 pytestmark = pytest.mark.gpu
-D, U = 128, 2.0 ** -8
+D, U, H = 128, 2.0 ** -8, 2.0 ** -11
+NORM = 2 * math.sqrt((U * U + 4 * H * H) / 3)
 
 
 def _axis_map(axes):
@@ -133,7 +134,7 @@ class Case:
                     out[mine][i, h] = p @ vv
                     mass[mine][i, h] = p @ vv.abs()
                     slack[mine][i, h] = (kk.abs() @ q[i, h].abs()).max() / math.sqrt(D)
-        return out, mass, 2 * U * slack
+        return out, mass, 2 * H * slack
 
     def check(self, got=None, masks=None):
         got = (self.out if got is None else got)[:self.N].double()
@@ -141,9 +142,10 @@ class Case:
         err = (got - want).abs()
         norm = float((got - want).norm() / want.norm().clamp(min=1e-300)) if float(want.norm()) else float(err.max())
         if self.out.dtype == torch.bfloat16:
-            fits = bool((err <= ((2 * d).exp() * (1 + U) ** 3 - 1) * mass + U * want.abs()).all())
+            before = ((2 * d).exp() * (1 + H) ** 3 - 1) * mass
+            fits = bool((err <= before + U * (want.abs() + before)).all())
             assert fits, float((err / mass.clamp(min=1e-30)).max())
-            assert norm <= 2 * 1.29 * U, norm
+            assert norm <= NORM, norm
         else:
             fits = bool((err <= 4 * 1.2e-5 * mass + 1e-30).all())
             assert fits, float((err / mass.clamp(min=1e-30)).max())
@@ -319,12 +321,14 @@ def test_lengths_and_offsets_beyond_what_the_host_said_are_cut():
     cv.commvq_destroy(h)
 
 
-def test_large_logits():
-    c = Case([900], [tree(6)], seed=15)
+@pytest.mark.parametrize("n,Hkv,k", [(900, 2, 6), (12400, 8, 3), (12400, 8, 7)])
+def test_large_logits(n, Hkv, k):
+    c = Case([n], [tree(k)], Hkv=Hkv, seed=15)
     c.q *= 30
     c.call()
     want, mass, d = c.plain()
-    fits = bool(((c.out.double() - want).abs() <= ((2 * d).exp() * (1 + U) ** 3 - 1) * mass + U * want.abs()).all())
+    before = ((2 * d).exp() * (1 + H) ** 3 - 1) * mass
+    fits = bool(((c.out.double() - want).abs() <= before + U * (want.abs() + before)).all())
     assert fits
 
 
@@ -386,7 +390,7 @@ def test_single_nodes_agree_with_decode_attention_of_the_flat_cache():
     c.base = w.rope_base
     c.call()
     c.check()
-    assert float((c.out.double() - flat.double()).norm() / flat.double().norm()) <= 2 * 1.29 * U
+    assert float((c.out.double() - flat.double()).norm() / flat.double().norm()) <= NORM
     op.close()
 
 
@@ -419,6 +423,16 @@ def test_long_ragged(most, block):
         c.more = sizes
         c.call()
         c.check()
+
+
+@pytest.mark.parametrize("axes", [1, 2])
+@pytest.mark.parametrize("k", [0, 40])
+def test_long_sequences_without_nodes_at_either_end(k, axes):
+    # (their first node's position would be in front of, or behind, what is there)
+    kw = {} if axes == 1 else dict(axes=2, key_pos=lambda gen, n, a: torch.randint(0, 9000, (n, a), generator=gen, device="cuda", dtype=torch.int32))
+    c = Case([5000, 9000, 3000, 0, 12000], [[], tree(5), tree(k), tree(3), []], Hkv=8, G=4, seed=k, **kw)
+    c.call()
+    c.check()
 
 
 @pytest.mark.parametrize("k", [4, 10, 40])
@@ -461,6 +475,17 @@ def test_long_codewords_that_no_counted_token_selects(k):
     c.key_pages[0], c.val_pages[0] = 0, 0
     c.table[0][c.table[0] == 0] = -1
     c.table[0, 1], c.table[0, 300], c.table[0, 500:640] = c.pool, 2 ** 31 - 1, -5
+    c.call()
+    c.check()
+
+
+@pytest.mark.parametrize("n,k", [(300, 3), (12500, 3), (12500, 18)])
+@pytest.mark.parametrize("keys,vals", [(2.0 ** 100, 2.0 ** -110), (2.0 ** -90, 2.0 ** 60), (1.0, 2.0 ** 30)])
+def test_codebooks_of_any_magnitude(n, k, keys, vals):
+    """Sizes that only bf16's exponents hold; queries make up for the keys'."""
+    c = Case([n], [tree(k)], Hkv=8, seed=k)
+    c.key_cb, c.node_k, c.q = c.key_cb * keys, c.node_k * keys, c.q / keys
+    c.val_cb, c.node_v = c.val_cb * vals, c.node_v * vals
     c.call()
     c.check()
 

@@ -55,6 +55,7 @@ def test_what_is_acceptable_stops_only_at_the_missing_device(planner):
     assert attn(h, tables=None) == NO_DEVICE
     assert attn(h, node_mask=None) == NO_DEVICE
     assert attn(h, max_seqlen=0) == NO_DEVICE
+    assert attn(h, total_tokens=5000) == NO_DEVICE and attn(h, total_tokens=10000) == NO_DEVICE
     assert attn(h, q_stride=48 * 128, node_stride=48 * 128) == NO_DEVICE
     assert attn(h, pages=cv.make_pages(1024, 1000, 400, 3), pair_axis=[0] * 16 + [1] * 24 + [2] * 24, key_pos=P) == NO_DEVICE
     assert attn(planner(q_dtype=0, codebook_dtype=0), tables=None) == NO_DEVICE
@@ -88,7 +89,7 @@ def test_pool_geometry(planner, pages):
 
 @pytest.mark.parametrize("kw", [dict(batch=0), dict(max_nodes=0), dict(max_nodes=65, total_nodes=70), dict(total_nodes=11), dict(total_nodes=25), dict(max_seqlen=-1),
                                 dict(max_seqlen=6401), dict(q_stride=4095), dict(q_stride=4100), dict(q_stride=8), dict(node_stride=1020), dict(node_stride=1028),
-                                dict(q_stride=-4096)])
+                                dict(q_stride=-4096), dict(total_tokens=-1), dict(total_tokens=4999), dict(total_tokens=10001)])
 def test_shapes(planner, kw):
     assert attn(planner(), **kw) == SHAPE
 
@@ -123,7 +124,7 @@ def test_workspace(planner):
     assert cv.commvq_tree_workspace_bytes(h, 1, 1, 1, 0) > 0
     for bad in ((0, 1, 1, 1), (1, 0, 1, 1), (1, 2, 1, 1), (1, 65, 65, 1), (1, 1, 1, -1)):
         assert status(cv.commvq_tree_workspace_bytes, h, *bad) == SHAPE
-    assert cv.commvq_tree_table_bytes(h) == 8 * (16 + 32) * 256 * 128 * 2
+    assert cv.commvq_tree_table_bytes(h) == 8 * (16 + 32) * 256 * 128 * 2 + 256   # and a power of two per head and kind
     assert status(cv.commvq_tree_prepare, h, P, P, P + 8) == SHAPE and status(cv.commvq_tree_prepare, h, None, P, P) == NULL
 
 
