@@ -120,3 +120,87 @@ class DecodeAttention:
         B.commvq_stage_output(self.handle, dw.val_codebooks, dw.positions, self.out, self.workspace,
                               self.workspace_bytes, st)
         return self.out
+
+
+class PagedCache:
+    """The pages of one layer for up to `batch` sequences: records in index form, block tables, free pages.
+
+    Lengths and the pages that a sequence owns are kept on the host; one object's calls belong on one stream."""
+
+    def __init__(self, cfg: B.Config, handle, n_blocks: int, block_size: int, batch: int, max_blocks: int, n_axes: int = 1):
+        torch = _torch()
+        self.cfg, self.handle, self.batch = cfg, handle, batch
+        self.pages = B.make_pages(block_size, n_blocks, max_blocks, n_axes)
+        heads = cfg.n_kv_heads
+        self.key_pages = torch.zeros((n_blocks, heads, block_size, cfg.m_key), dtype=torch.uint8, device="cuda")
+        self.val_pages = torch.zeros((n_blocks, heads, block_size, cfg.m_val), dtype=torch.uint8, device="cuda")
+        self.key_pos = torch.zeros((n_blocks * block_size, n_axes), dtype=torch.int32, device="cuda") if n_axes > 1 else None
+        self.block_tables = torch.full((batch, max_blocks), -1, dtype=torch.int32, device="cuda")
+        self.seq_lens = torch.zeros(batch, dtype=torch.int32, device="cuda")
+        self.lens = [0] * batch
+        self.free = list(range(n_blocks))
+        self.owned = [[] for _ in range(batch)]
+
+    def append(self, new_lens, key_codes, val_codes, token_pos=None):
+        """Takes pages for new_lens[b] more tokens of every sequence and stores their records, [sum of new_lens][heads][codebooks], sequence by sequence."""
+        torch = _torch()
+        size, total = self.pages.block_size, sum(new_lens)
+        pages_of = lambda n: -(-n // size)
+        if len(new_lens) != self.batch or min(new_lens) < 0:
+            raise ValueError("new_lens: one number >= 0 per sequence")
+        want = [pages_of(c + n) - pages_of(c) for c, n in zip(self.lens, new_lens)]
+        need = sum(want)
+        if need > len(self.free) or any(pages_of(c + n) > self.pages.max_blocks for c, n in zip(self.lens, new_lens)):
+            raise RuntimeError("the cache has no room for the new tokens")
+        ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+        stream = int(torch.cuda.current_stream().cuda_stream)
+        cached, new, free = ints(self.lens), ints(list(new_lens)), ints(self.free[:need] or [-1])
+        cu, slots, taken = (torch.empty(n, dtype=torch.int32, device="cuda") for n in (self.batch + 1, max(1, total), 2))
+        B.commvq_page_tables(self.pages, self.batch, cached, new, free, need, self.block_tables, self.seq_lens, cu, slots, None, total, taken, stream)
+        if total:
+            B.commvq_store_pages(self.handle, self.pages, total, slots, key_codes, val_codes, token_pos if self.key_pos is not None else None,
+                                 self.key_pages, self.val_pages, self.key_pos, stream)
+        for b, n in enumerate(want):
+            self.owned[b] += self.free[:n]
+            del self.free[:n]
+        self.lens = [c + n for c, n in zip(self.lens, new_lens)]
+        return slots
+
+    def release(self, b: int):
+        """Sequence b is done: its pages are free again, its place is empty."""
+        self.free += self.owned[b]
+        self.owned[b], self.lens[b] = [], 0
+        self.seq_lens[b] = 0
+
+
+class TreeAttention:
+    """Attention of drafted trees over a PagedCache: the layer's codebooks, laid out once, and a workspace that grows with the batch.
+
+    One object's calls belong on one stream (they share the workspace)."""
+
+    def __init__(self, cfg: B.Config, handle, key_codebooks, val_codebooks):
+        torch = _torch()
+        self.cfg, self.handle, self.key_codebooks, self.val_codebooks = cfg, handle, key_codebooks, val_codebooks
+        self.tables = None
+        if cfg.codebook_dtype == B.COMMVQ_BF16:
+            self.tables = torch.empty(B.commvq_tree_table_bytes(handle), dtype=torch.uint8, device="cuda")
+            B.commvq_tree_prepare(handle, key_codebooks, val_codebooks, self.tables, int(torch.cuda.current_stream().cuda_stream))
+        self.workspace = torch.empty(0, dtype=torch.uint8, device="cuda")
+
+    def __call__(self, cache: PagedCache, q, node_keys, node_vals, nodes, node_pos, node_mask=None, pair_axis=None, out=None):
+        """nodes[b]: drafted tokens of sequence b (host); the other arguments are the call's device tensors."""
+        torch = _torch()
+        total, most, longest = sum(nodes), max(nodes), max(cache.lens)
+        ends = [0]
+        for n in nodes:
+            ends.append(ends[-1] + n)
+        cu = torch.tensor(ends, dtype=torch.int32, device="cuda")
+        need = B.commvq_tree_workspace_bytes(self.handle, cache.batch, total, most, longest)
+        if self.workspace.numel() < need:
+            self.workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
+        out = torch.empty_like(q) if out is None else out
+        tree = B.make_tree(cache.batch, total, most, longest, cache.seq_lens, cache.block_tables, cu, node_pos, node_mask, cache.key_pos, pair_axis,
+                           total_tokens=sum(cache.lens))
+        B.commvq_tree_attn(self.handle, cache.pages, tree, q, node_keys, node_vals, cache.key_pages, cache.val_pages, self.key_codebooks,
+                           self.val_codebooks, self.tables, out, self.workspace, self.workspace.numel(), int(torch.cuda.current_stream().cuda_stream))
+        return out
