@@ -418,7 +418,8 @@ commvq_status commvq_store_pages(commvq_handle *handle, const commvq_pages *page
  *   key_pages, val_pages as above;  key_codebooks, val_codebooks  as for commvq_decode_attn in index form
  *   tables               what commvq_tree_prepare made of the codebooks, or NULL: rows are then gathered from the codebooks,
  *                        whatever the context's length (long ones are several times faster with tables)
- *   workspace            >= commvq_tree_workspace_bytes(...) bytes, 256-byte aligned, contents undefined after
+ *   workspace            >= commvq_tree_workspace_bytes(...) bytes, 256-byte aligned, contents undefined after (sizes do not only
+ *                        grow: a smaller batch may be split further, so ask for every size that is used)
  * All data pointers are 16-byte aligned, strides multiples of 8 elements.  Distances between any two positions of a sequence (node or
  * token, on one axis) must not exceed max_position; beyond, rotations are wrong, but nothing faults.  position_free handles turn nothing.
  * bf16 queries with bf16 codebooks: turned queries and keys, softmax weights and values enter the products as fp16 times powers of

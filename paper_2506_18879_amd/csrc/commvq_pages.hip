@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kTableThreads) void k_page_tables(TableArgs a)
         const int b = b0 + tid;
         const long long cached = b < a.batch ? max(a.cached[b], 0) : 0, fresh = b < a.batch ? max(a.fresh[b], 0) : 0;
         const long long held = (cached + page_mask) >> a.block_bits, after = (cached + fresh + page_mask) >> a.block_bits;
-        const bool fits = after <= a.max_blocks;
+        const bool fits = after <= a.max_blocks && cached + fresh <= 0x7fffffff;
         Sums total;
         const Sums own = {fresh, fits ? after - held : 0};
         const Sums at = scan_exclusive(own, waves, total);

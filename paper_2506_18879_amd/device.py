@@ -122,6 +122,12 @@ class DecodeAttention:
         return self.out
 
 
+def _expect(name: str, t, shape, dtype):
+    """The calls take addresses: a tensor of another shape, type, order or place would be misread."""
+    if t is None or tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} on the GPU")
+
+
 class PagedCache:
     """The pages of one layer for up to `batch` sequences: records in index form, block tables, free pages.
 
@@ -152,6 +158,11 @@ class PagedCache:
         need = sum(want)
         if need > len(self.free) or any(pages_of(c + n) > self.pages.max_blocks for c, n in zip(self.lens, new_lens)):
             raise RuntimeError("the cache has no room for the new tokens")
+        if total:
+            _expect("key_codes", key_codes, (total, self.cfg.n_kv_heads, self.cfg.m_key), torch.uint8)
+            _expect("val_codes", val_codes, (total, self.cfg.n_kv_heads, self.cfg.m_val), torch.uint8)
+            if self.key_pos is not None:
+                _expect("token_pos", token_pos, (total, self.pages.n_axes), torch.int32)
         ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
         stream = int(torch.cuda.current_stream().cuda_stream)
         cached, new, free = ints(self.lens), ints(list(new_lens)), ints(self.free[:need] or [-1])
@@ -191,6 +202,19 @@ class TreeAttention:
         """nodes[b]: drafted tokens of sequence b (host); the other arguments are the call's device tensors."""
         torch = _torch()
         total, most, longest = sum(nodes), max(nodes), max(cache.lens)
+        if len(nodes) != cache.batch or min(nodes) < 0:
+            raise ValueError("nodes: one number >= 0 per sequence")
+        kind = torch.bfloat16 if self.cfg.q_dtype == B.COMMVQ_BF16 else torch.float32
+        _expect("q", q, (total, self.cfg.n_q_heads, 128), kind)
+        _expect("node_keys", node_keys, (total, self.cfg.n_kv_heads, 128), kind)
+        _expect("node_vals", node_vals, (total, self.cfg.n_kv_heads, 128), kind)
+        _expect("node_pos", node_pos, (total, cache.pages.n_axes), torch.int32)
+        if node_mask is not None:
+            _expect("node_mask", node_mask, (total,), torch.int64)
+        if out is not None:
+            _expect("out", out, tuple(q.shape), kind)
+        if total == 0:
+            return torch.empty_like(q) if out is None else out
         ends = [0]
         for n in nodes:
             ends.append(ends[-1] + n)

@@ -17,7 +17,7 @@ def plain(block, n_blocks, cached, new, free, table, n_slots):
     for b, (c, n) in enumerate(zip(cached, new)):
         c, n = max(c, 0), max(n, 0)
         held, after = -(-c // block), -(-(c + n) // block)
-        fits = after <= width
+        fits = after <= width and c + n < 2 ** 31
         need = after - held if fits else 0
         ok = fits and (need == 0 or asked + need <= len(free)) and first + n <= n_slots
         if ok:
@@ -103,6 +103,7 @@ def test_pages_outside_the_pool_and_lengths_that_overflow():
     big = 2 ** 31 - 1
     d, _, want = run(16, 10, [big - 3, 5, big], [0, 2, 0], [1], [[1, 2]] * 3, 4)
     assert d["lens"].tolist() == [big - 3, 7, big]
+    run(1024, 10, [big - 5, 5], [10, 2], [1, 2], [[0] * (2 ** 21 + 1)] * 2, 16)   # a length that 32 bits do not hold, in a row that is long enough
 
 
 def test_positions_are_optional_and_calls_repeat():

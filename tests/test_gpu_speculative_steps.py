@@ -105,6 +105,13 @@ def test_prompts_drafts_and_accepted_paths(prompts, drafts, axes):
             append([(normal(n, Hkv, D), normal(n, Hkv, D), place(n, 0)) for n in [prompts[0] // 2] + [0] * (B - 1)])
     with pytest.raises(RuntimeError):
         cache.append([10 ** 6] + [0] * (B - 1), None, None)
-    with pytest.raises(ValueError):
-        cache.append([-1] + [0] * (B - 1), None, None)
+    codes = torch.zeros((2, Hkv, M), dtype=torch.uint8, device="cuda")
+    one = [1] + [0] * (B - 1)
+    for new, k, v in (([-1] + [0] * (B - 1), None, None), (one, codes, codes), (one, codes[:1], None), (one, codes[:1].int(), codes[:1]), ([1], codes[:1], codes[:1])):
+        with pytest.raises(ValueError):
+            cache.append(new, k, v, place(1, 0).cuda())
+    assert attn(cache, q[:0], nk[:0], nv[:0], [0] * B, pos[:0].cuda()).shape == (0, Hkv * G, D)
+    for bad in (q.float(), q[:-1], q.transpose(0, 1).contiguous().transpose(0, 1), q.cpu()):
+        with pytest.raises(ValueError):
+            attn(cache, bad, nk, nv, drafts, pos.cuda())
     cv.commvq_destroy(h)
