@@ -378,15 +378,16 @@ typedef struct {
  * Block tables and slots from the requests' lengths, on the GPU.  Request b holds cached_lens[b] tokens in
  * ceil(cached / block_size) pages and gets new_lens[b] more; pages that it lacks are taken from the front of free_blocks, request
  * by request.  A request is granted if its row and what is left of the list are long enough (the pages asked for by the
- * requests before it count whether they were granted or not, so that the order of grants is that of the requests) and if its tokens
- * end at or before n_slots; a request that is not granted keeps its row and its length, and its new tokens have no slot.
+ * requests before it count whether they were granted or not, so that the order of grants is that of the requests), if its new
+ * length is below 2^31 and if its tokens end at or before n_slots; a request that is not granted keeps its row and its length, and
+ * its new tokens have no slot.
  *   cached_lens, new_lens  device [B] (negative numbers count as 0)
  *   free_blocks            device [n_free] (NULL if n_free is 0)
  *   block_tables           device [B][max_blocks], in/out: entries of new pages are written, all others left as they were
  *   seq_lens               device [B] out: cached + new where granted, cached otherwise
  *   cu_new                 device [B+1] out: prefix sums of new_lens (of granted and other requests)
  *   slots                  device [n_slots] out: slot of every new token, request by request; -1 without one, and behind the last token
- *   token_pos              device [n_slots] out or NULL: index of every new token in its sequence; behind the last one left as it was
+ *   token_pos              device [n_slots] out or NULL: index of every new token in its sequence (2^31 - 1 at most); behind the last one left as it was
  *   taken                  device [2] out: pages taken, requests not granted
  * Outputs must not overlap inputs (block_tables apart).  No handle and no workspace; n_axes is not looked at.
  */

